@@ -292,6 +292,107 @@ int cmp_estimate_eb(cmp_ctx *ctx, const float *d_act, uint64_t act_numel, const 
                     uint64_t per_sample, const float *d_mom, uint64_t mom_numel, const cmp_controller_config *cfg,
                     float *h_eb, double *h_stats, void *stream);
 
+/* ---- Activations in eight bits -----------------------------------------------------------------
+ *
+ * The codec above needs what the activations of convolutional networks have: zeros and smooth planes.
+ * The entry points below hold any activation (bf16, fp16 or fp32, dense or not) with eight bits per value, and
+ * compute a layer's backward pass from that form, so that the restored tensor never exists in memory (the
+ * framework of Section 4.4, compress in the forward pass and restore in the backward pass, with another codec).
+ * They take no context: they allocate nothing, keep nothing between calls and do not synchronise, so calls on
+ * different streams are independent as long as their buffers are, and every call can be captured into a graph.
+ * `device` is the GPU of the buffers and of `stream` (it need not be the current one).  No launch depends on
+ * device data.  Same inputs, same bytes and values on every run.
+ *
+ * Byte checkpoint of x[rows][cols]: the columns of every row in groups of `group` (32, 64 or 128; the last group of a
+ * row may be shorter), every group with a scale 2^e.  With amax the largest FINITE magnitude of the group,
+ *    CMP_BYTE_INT    e: the smallest with amax <= 127.5 * 2^e, in [-110, 121]; code = x * 2^-e rounded to
+ *                    nearest even and clamped to -127..127 (int8); -128 stands for NaN and infinities;
+ *    CMP_BYTE_FLOAT  e: the smallest with amax <= 448 * 2^e, in [-110, 119]; code = x * 2^-e rounded to nearest
+ *                    even to e4m3 (4 exponent bits, bias 7, 3 mantissa bits, largest 448, 0x7f and 0xff NaN); NaN for
+ *                    NaN and infinities;
+ *    x' = code * 2^e in both.
+ * So |x - x'| <= 2^(e-1) (CMP_BYTE_INT: at most amax / 127), or <= max(|x| / 16, 2^(e-10)) (CMP_BYTE_FLOAT);
+ * a group whose e is cut off at the upper end (amax above 1.6e38 or 1.5e38 only) saturates at its largest code instead.
+ * x' has at most eight significant bits: it is a bf16 number exactly.
+ * The bytes, in one buffer aligned to 16:
+ *    codes  rows * pitch, pitch = cols rounded up to 16; the padding behind a row is zero
+ *    exps   rows * ceil(cols / group) bytes e + 127, then zeros up to a multiple of 16.
+ * Any bytes decode to something: a damaged checkpoint gives wrong values, never an access out of bounds. */
+#define CMP_TYPE_F     0u    /* fp32 */
+#define CMP_TYPE_H     1u    /* fp16 */
+#define CMP_TYPE_BF    2u    /* bf16 */
+#define CMP_BYTE_INT   0u
+#define CMP_BYTE_FLOAT 1u
+
+typedef struct {
+    uint64_t rows, cols;     /* each at most 2^31 - 1; 0 is allowed (an empty checkpoint) */
+    uint32_t format;         /* CMP_BYTE_INT or CMP_BYTE_FLOAT */
+    uint32_t group;          /* 32, 64 or 128 */
+} cmp_byte_shape;
+
+/* Bytes of a checkpoint (a multiple of 16); 0 on a bad shape, and for an empty one. */
+size_t cmp_byte_bytes(const cmp_byte_shape *shape);
+
+/* Stores d_x (element type `type`, rows `ld` >= cols elements apart, aligned to its element) into d_ck of `cap` bytes,
+ * and restores it.  A restored value beyond the largest finite one of `type` (fp16 only) becomes that value.
+ * cmp_byte_load writes the cols elements of every row and nothing between rows.  CMP_E_NOSPACE: cap too small;
+ * CMP_E_FORMAT: `bytes` cannot hold a checkpoint of this shape; CMP_E_ARG otherwise. */
+int cmp_byte_store(int device, const cmp_byte_shape *shape, const void *d_x, uint32_t type, uint64_t ld, void *d_ck, size_t cap,
+                   void *stream);
+int cmp_byte_load(int device, const cmp_byte_shape *shape, const void *d_ck, size_t bytes, void *d_out, uint32_t type, uint64_t ld,
+                  void *stream);
+
+/* Weight and bias gradient of a linear layer y = x W^T + b whose input x[rows][cols] is held as a byte checkpoint:
+ *    dW[n][k] = sum over m of dY[m][n] * x'[m][k],     db[n] = sum over m of dY[m][n]     (n < outs, k < cols)
+ * dY[rows][outs] of element type `type`, rows ld_dy >= outs elements apart; dW contiguous, dW and db of type out_type:
+ * `type` or CMP_TYPE_F.  d_db may be NULL.  accumulate != 0 adds to what dW and db hold.  All products are exact and
+ * summed in fp32 (fp16 and fp32 values of dY enter as the sum of two or three bf16 numbers, parts below 2^-126 may
+ * be lost); each result is rounded once to out_type.  rows = 0 gives zeros.
+ * d_work: cmp_byte_linear_grad_work bytes (it may be 0), aligned to 16, used during the call only; too few bytes
+ * are CMP_E_NOSPACE.  More than 2^23 tiles of 128 x 128 in dW are refused (CMP_E_ARG). */
+size_t cmp_byte_linear_grad_work(const cmp_byte_shape *shape, uint64_t outs, uint32_t type);
+int cmp_byte_linear_grad(int device, const cmp_byte_shape *shape, const void *d_ck, size_t bytes, const void *d_dy, uint32_t type,
+                         uint64_t outs, uint64_t ld_dy, void *d_dw, void *d_db, uint32_t out_type, int accumulate, void *d_work,
+                         size_t work_bytes, void *stream);
+
+/* Group norm with an activation, channels last: x[batch][spatial][channels], contiguous,
+ *    h = (x - mean) / sqrt(var + eps),  y = act(h * gamma + beta)
+ * with mean and (biased) variance over the positions and the channels / groups consecutive channels of a group.
+ * d_gamma, d_beta: fp32, one per channel, either may be NULL (ones, zeros).  d_stats (double, [batch][groups][2]: mean,
+ * 1 / sqrt(var + eps)) is written for the backward pass; NULL: not wanted.  With d_ck the input is kept as a byte
+ * checkpoint of batch * spatial rows in the same pass, the bytes of cmp_byte_store; NULL: not kept.
+ * d_work: cmp_group_norm_work bytes, aligned to 16, used during a call only, the same for both directions.
+ * cmp_group_norm_grad takes the input d_x OR its checkpoint d_ck (the other NULL), gamma, beta and d_stats of
+ * the forward pass, and gives, with u = h * gamma + beta from the restored input and du = dy * act'(u),
+ *    dbeta = sum du,  dgamma = sum du * h   (fp32, overwritten; either may be NULL)
+ *    dx = (du * gamma - (A + h * B) / count) / sqrt(var + eps),  A, B: sums of du * gamma, du * gamma * h over a group.
+ * The statistics are those of the input itself, so the error of a code enters h divided by the group's deviation: a norm
+ * whose deviation is not well above the steps 2^e of its checkpoint (groups of a few equal values, channels of very
+ * different sizes in one scale group) is better kept as d_x.  The derivative of CMP_ACT_RELU at 0 is 0.  Sums run over fp32 or fp64 in an order that the sizes fix.
+ * A NaN or an infinity in x spoils its group, as the formulas have it.  With batch or spatial 0 nothing is written
+ * but zeros in dgamma and dbeta.  d_y must not overlap d_x, nor d_dx d_dy. */
+#define CMP_ACT_NONE 0u
+#define CMP_ACT_RELU 1u
+#define CMP_ACT_SILU 2u      /* u / (1 + exp(-u)) */
+#define CMP_NORM_MAX_CHANNELS 8192u
+#define CMP_NORM_MAX_GROUPS   4096u
+#define CMP_NORM_MAX_BATCH    (1u << 21)
+
+typedef struct {
+    uint64_t batch, spatial;         /* batch * spatial at most 2^31 - 1 */
+    uint32_t channels, groups;       /* groups divides channels */
+    uint32_t type, act;
+    double   eps;                    /* > 0, finite */
+} cmp_norm_shape;
+
+size_t cmp_group_norm_work(const cmp_norm_shape *shape);
+int cmp_group_norm(int device, const cmp_norm_shape *shape, const void *d_x, const float *d_gamma, const float *d_beta, void *d_y,
+                   double *d_stats, uint32_t format, uint32_t group, void *d_ck, size_t cap, void *d_work, size_t work_bytes,
+                   void *stream);
+int cmp_group_norm_grad(int device, const cmp_norm_shape *shape, const void *d_dy, const void *d_x, uint32_t format, uint32_t group,
+                        const void *d_ck, size_t bytes, const float *d_gamma, const float *d_beta, const double *d_stats, void *d_dx,
+                        float *d_dgamma, float *d_dbeta, void *d_work, size_t work_bytes, void *stream);
+
 /* A static English string for a return code of this library (the conditions listed at the top:
  * what broke the guarantee of Section 2.2 or the container of Section 3.1); never NULL. */
 const char *cmp_strerror(int code);

@@ -11,6 +11,10 @@ so neither hook ever waits for the GPU: compression runs behind the forward pass
 
 Nothing here computes: both hooks marshal arguments for the C ABI.  Parameters, tensors that are
 not fp32 4-D CUDA tensors, small tensors and shapes the stack does not take are saved as they are.
+
+What that codec does not take or does not shrink (bf16 and fp16, dense activations, channels last) can be held with
+eight bits per value instead: :class:`ByteCheckpoints` are hooks of the same kind over byte checkpoints, and
+:func:`linear` and :func:`group_norm` are layers whose backward pass reads the eight-bit form itself.
 """
 from __future__ import annotations
 
@@ -20,7 +24,7 @@ from typing import Callable, Iterable, Optional, Union
 
 import torch
 
-from . import binding
+from . import binding, operators
 
 
 class SlotStack:
@@ -168,3 +172,127 @@ class ActivationCompressor:
         if st < 0:
             raise binding.CmpError(st, "activation stack")
         return {"top": top, "peak": peak, "held": held, "status": st}
+
+
+@dataclass
+class _HeldBytes:
+    """What autograd holds instead of a tensor: its checkpoint in the order of its memory, and that order."""
+    ck: operators.ByteCheckpoint
+    order: tuple
+
+
+class ByteCheckpoints:
+    """saved_tensors_hooks that hold every saved fp32, fp16 or bf16 tensor as a byte checkpoint, whatever its shape and
+    whatever the order of its dimensions in memory (channels last included; groups run along the dimension that is
+    dense).  A graph can be walked backward as often as autograd allows: checkpoints are only read.
+
+    fmt, group: see operators.byte_store.  min_numel: smaller tensors are saved as they are, and so are parameters,
+    tensors named to skip_parameters and tensors with gaps.  A value is off by at most 1/127 of the largest in its group
+    ("int8") or 1/16 of itself ("e4m3"): what is not an activation (indices kept as floats, running sums) does not
+    belong under these hooks.
+    """
+
+    def __init__(self, fmt: str = "int8", group: int = 64, min_numel: int = 1 << 14):
+        operators._byte_shape(0, 0, fmt, group)                       # refuses what byte_store would refuse later
+        self.fmt, self.group, self.min_numel = fmt, int(group), int(min_numel)
+        self._skip = set()
+        self.stats = {"packed": 0, "raw_bytes": 0, "held_bytes": 0, "passed_through": 0}
+
+    def skip_parameters(self, params: Iterable[torch.Tensor]) -> None:
+        for p in params:
+            self._skip.add(p.data_ptr())
+
+    def pack(self, t: torch.Tensor):
+        order = tuple(sorted(range(t.dim()), key=lambda d: (-t.stride(d), d)))
+        if (not t.is_cuda or t.dtype not in operators._TYPES or t.dim() < 1 or t.numel() < max(1, self.min_numel)
+                or isinstance(t, torch.nn.Parameter) or t.data_ptr() in self._skip or not t.permute(order).is_contiguous()):
+            self.stats["passed_through"] += 1
+            return t
+        ck = operators.byte_store(t.detach().permute(order), self.fmt, self.group)
+        self.stats["packed"] += 1
+        self.stats["raw_bytes"] += t.numel() * t.element_size()
+        self.stats["held_bytes"] += ck.nbytes
+        return _HeldBytes(ck, order)
+
+    def unpack(self, h):
+        if not isinstance(h, _HeldBytes):
+            return h
+        back = [0] * len(h.order)
+        for i, d in enumerate(h.order):
+            back[d] = i
+        return operators.byte_load(h.ck).permute(back)
+
+    def hooks(self):
+        """Context manager for one forward pass: ``with held.hooks(): loss = model(x)``."""
+        return torch.autograd.graph.saved_tensors_hooks(self.pack, self.unpack)
+
+
+def _dense_rows(t: torch.Tensor) -> torch.Tensor:
+    """t, or a copy where its rows are not evenly spaced (the gradient of a sum comes as one expanded value)."""
+    return t if operators._rows_of(t) is not None else t.contiguous()
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    @torch.amp.custom_fwd(device_type="cuda")
+    def forward(ctx, x, weight, bias, fmt, group):
+        ctx.held = operators.byte_store(_dense_rows(x), fmt, group) if ctx.needs_input_grad[1] else None
+        ctx.save_for_backward(weight if ctx.needs_input_grad[0] else None)
+        ctx.kinds = (x.dtype, weight.dtype, None if bias is None else bias.dtype)
+        return torch.nn.functional.linear(x, weight, bias)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    @torch.amp.custom_bwd(device_type="cuda")
+    def backward(ctx, dy):
+        (weight,) = ctx.saved_tensors
+        dx = dw = db = None
+        if ctx.needs_input_grad[0]:
+            dx = torch.matmul(dy, weight.to(dy.dtype)).to(ctx.kinds[0])
+        with_bias = ctx.kinds[2] is not None and ctx.needs_input_grad[2]
+        if ctx.needs_input_grad[1]:
+            dtype = torch.float32 if ctx.kinds[1] == torch.float32 else dy.dtype
+            dw, db = operators.byte_linear_grad(_dense_rows(dy), ctx.held, bias=with_bias, dtype=dtype)
+            dw = dw.to(ctx.kinds[1])
+        elif with_bias:
+            db = dy.reshape(-1, dy.shape[-1]).sum(0, dtype=torch.float32)
+        if db is not None:
+            db = db.to(ctx.kinds[2])
+        return dx, dw, db, None, None
+
+
+def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, fmt: str = "int8", group: int = 64):
+    """torch.nn.functional.linear whose input is held as a byte checkpoint; the weight's (and bias's) gradient is computed from
+    the eight-bit form by operators.byte_linear_grad.  x: [..., cols] in float32, float16 or bfloat16 on a GPU."""
+    return _Linear.apply(x, weight, bias, fmt, group)
+
+
+class _GroupNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, groups, eps, act, fmt, group):
+        x = x.contiguous()
+        w, b = (None if p is None else p.float().contiguous() for p in (weight, bias))
+        y, stats, held = operators.group_norm(x, groups, w, b, eps, act, save=fmt, group=group)
+        ctx.held, ctx.groups, ctx.act = held, groups, act
+        ctx.kinds = tuple(None if p is None else p.dtype for p in (weight, bias))
+        ctx.save_for_backward(w, b, stats, None if held is not None else x)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        w, b, stats, x = ctx.saved_tensors
+        params = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
+        dx, dw, db = operators.group_norm_grad(dy.contiguous(), ctx.held if x is None else x, stats, ctx.groups, w, b, ctx.act,
+                                               params=params)
+        dw = dw.to(ctx.kinds[0]) if params and ctx.needs_input_grad[1] else None
+        db = db.to(ctx.kinds[1]) if params and ctx.needs_input_grad[2] else None
+        return dx if ctx.needs_input_grad[0] else None, dw, db, None, None, None, None, None
+
+
+def group_norm(x: torch.Tensor, groups: int, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+               eps: float = 1e-5, act: str = "none", fmt: Optional[str] = "int8", group: int = 64):
+    """Group norm and activation of x[batch, ..., channels] (channels last: permute an NCHW tensor to NHWC first, which costs
+    nothing for one in torch's channels_last format).  Its input is held as a byte checkpoint written in the same pass;
+    fmt=None holds x itself."""
+    return _GroupNorm.apply(x, weight, bias, groups, eps, act, fmt, group)

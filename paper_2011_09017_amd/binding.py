@@ -20,12 +20,17 @@ CMP_OK, CMP_E_ARG, CMP_E_NOSPACE, CMP_E_FORMAT, CMP_E_MISMATCH, CMP_E_HIP, CMP_W
 CMP_STAGE_QUANT_CODES, CMP_STAGE_HIST, CMP_STAGE_LENS, CMP_STAGE_CODES = 0, 1, 2, 3
 CMP_STAGE_OUTLIER_IDX, CMP_STAGE_OUTLIER_VAL = 4, 5
 CMP_F_ZERO_BLOCKS = 1
+CMP_TYPE_F, CMP_TYPE_H, CMP_TYPE_BF = 0, 1, 2
+CMP_BYTE_INT, CMP_BYTE_FLOAT = 0, 1
+CMP_ACT_NONE, CMP_ACT_RELU, CMP_ACT_SILU = 0, 1, 2
 
 EXPORTS = ["cmp_default_config", "cmp_create", "cmp_destroy", "cmp_bound", "cmp_compress",
            "cmp_compressed_size", "cmp_decompress", "cmp_last_status", "cmp_debug_stage", "cmp_strerror",
            "cmp_profile", "cmp_profile_read", "cmp_default_controller_config", "cmp_estimate_eb",
            "cmp_compress_begin", "cmp_compress_finish", "cmp_compress_batch", "cmp_decompress_batch", "cmp_compress_static",
-           "cmp_arena_state_bytes", "cmp_arena_accepts", "cmp_arena_init", "cmp_arena_push", "cmp_arena_pop", "cmp_arena_stats"]
+           "cmp_arena_state_bytes", "cmp_arena_accepts", "cmp_arena_init", "cmp_arena_push", "cmp_arena_pop", "cmp_arena_stats",
+           "cmp_byte_bytes", "cmp_byte_store", "cmp_byte_load", "cmp_byte_linear_grad_work", "cmp_byte_linear_grad",
+           "cmp_group_norm_work", "cmp_group_norm", "cmp_group_norm_grad"]
 
 
 class cmp_controller_config(C.Structure):
@@ -36,6 +41,15 @@ class cmp_config(C.Structure):
     _fields_ = [("radius", C.c_uint32), ("chunk", C.c_uint32), ("sub", C.c_uint32),
                 ("guard_shift", C.c_uint32), ("max_numel", C.c_uint64), ("flags", C.c_uint32),
                 ("reserved", C.c_uint32)]
+
+
+class cmp_byte_shape(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("cols", C.c_uint64), ("format", C.c_uint32), ("group", C.c_uint32)]
+
+
+class cmp_norm_shape(C.Structure):
+    _fields_ = [("batch", C.c_uint64), ("spatial", C.c_uint64), ("channels", C.c_uint32), ("groups", C.c_uint32),
+                ("type", C.c_uint32), ("act", C.c_uint32), ("eps", C.c_double)]
 
 
 _lib = None
@@ -78,6 +92,17 @@ def lib() -> C.CDLL:
         L.cmp_estimate_eb.restype = i32
         L.cmp_profile.argtypes = [vp, i32]; L.cmp_profile.restype = i32
         L.cmp_profile_read.argtypes = [vp, vp, i32, vp, vp, vp]; L.cmp_profile_read.restype = i32
+        u32, u64 = C.c_uint32, C.c_uint64
+        L.cmp_byte_bytes.argtypes = [vp]; L.cmp_byte_bytes.restype = sz
+        L.cmp_byte_store.argtypes = [i32, vp, vp, u32, u64, vp, sz, vp]; L.cmp_byte_store.restype = i32
+        L.cmp_byte_load.argtypes = [i32, vp, vp, sz, vp, u32, u64, vp]; L.cmp_byte_load.restype = i32
+        L.cmp_byte_linear_grad_work.argtypes = [vp, u64, u32]; L.cmp_byte_linear_grad_work.restype = sz
+        L.cmp_byte_linear_grad.argtypes = [i32, vp, vp, sz, vp, u32, u64, u64, vp, vp, u32, i32, vp, sz, vp]
+        L.cmp_byte_linear_grad.restype = i32
+        L.cmp_group_norm_work.argtypes = [vp]; L.cmp_group_norm_work.restype = sz
+        L.cmp_group_norm.argtypes = [i32, vp, vp, vp, vp, vp, vp, u32, u32, vp, sz, vp, sz, vp]; L.cmp_group_norm.restype = i32
+        L.cmp_group_norm_grad.argtypes = [i32, vp, vp, vp, u32, u32, vp, sz, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.cmp_group_norm_grad.restype = i32
         _lib = L
     return _lib
 
@@ -248,6 +273,45 @@ def cmp_estimate_eb(ctx, d_act: int, act_numel: int, d_loss: int, batch_n: int, 
     rc = lib().cmp_estimate_eb(ctx, d_act, act_numel, d_loss, batch_n, per_sample, d_mom, mom_numel,
                                C.addressof(cfg) if cfg is not None else None, C.addressof(eb), C.addressof(stats), stream)
     return rc, float(eb.value), (stats[0], stats[1], stats[2])
+
+
+def cmp_byte_bytes(shape: cmp_byte_shape) -> int:
+    return int(lib().cmp_byte_bytes(C.addressof(shape)))
+
+
+def cmp_byte_store(device: int, shape: cmp_byte_shape, d_x: int, type: int, ld: int, d_ck: int, cap: int, stream: int) -> int:
+    return lib().cmp_byte_store(device, C.addressof(shape), d_x, type, ld, d_ck, cap, stream)
+
+
+def cmp_byte_load(device: int, shape: cmp_byte_shape, d_ck: int, nbytes: int, d_out: int, type: int, ld: int, stream: int) -> int:
+    return lib().cmp_byte_load(device, C.addressof(shape), d_ck, nbytes, d_out, type, ld, stream)
+
+
+def cmp_byte_linear_grad_work(shape: cmp_byte_shape, outs: int, type: int) -> int:
+    return int(lib().cmp_byte_linear_grad_work(C.addressof(shape), outs, type))
+
+
+def cmp_byte_linear_grad(device: int, shape: cmp_byte_shape, d_ck: int, nbytes: int, d_dy: int, type: int, outs: int, ld_dy: int,
+                         d_dw: int, d_db: "int | None", out_type: int, accumulate: bool, d_work: int, work_bytes: int,
+                         stream: int) -> int:
+    return lib().cmp_byte_linear_grad(device, C.addressof(shape), d_ck, nbytes, d_dy, type, outs, ld_dy, d_dw, d_db, out_type,
+                                      1 if accumulate else 0, d_work, work_bytes, stream)
+
+
+def cmp_group_norm_work(shape: cmp_norm_shape) -> int:
+    return int(lib().cmp_group_norm_work(C.addressof(shape)))
+
+
+def cmp_group_norm(device: int, shape: cmp_norm_shape, d_x: int, d_gamma, d_beta, d_y: int, d_stats, format: int, group: int, d_ck,
+                   cap: int, d_work: int, work_bytes: int, stream: int) -> int:
+    return lib().cmp_group_norm(device, C.addressof(shape), d_x, d_gamma, d_beta, d_y, d_stats, format, group, d_ck, cap, d_work,
+                                work_bytes, stream)
+
+
+def cmp_group_norm_grad(device: int, shape: cmp_norm_shape, d_dy: int, d_x, format: int, group: int, d_ck, nbytes: int, d_gamma,
+                        d_beta, d_stats: int, d_dx: int, d_dgamma, d_dbeta, d_work: int, work_bytes: int, stream: int) -> int:
+    return lib().cmp_group_norm_grad(device, C.addressof(shape), d_dy, d_x, format, group, d_ck, nbytes, d_gamma, d_beta, d_stats,
+                                     d_dx, d_dgamma, d_dbeta, d_work, work_bytes, stream)
 
 
 def cmp_strerror(code: int) -> str:

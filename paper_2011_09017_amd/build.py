@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcmpz.so")
 SOURCES = ["cmpz_api.hip", "cmpz_compress.hip", "cmpz_sweep1.hip", "cmpz_codebook.hip", "cmpz_pack.hip", "cmpz_decompress.hip", "cmpz_decode_fused.hip",
-           "cmpz_controller.hip"]
+           "cmpz_controller.hip", "cmpz_byte_api.hip", "cmpz_byte.hip", "cmpz_linear_grad.hip", "cmpz_group_norm.hip"]
 
 # -ffp-contract=off: the quantiser multiplies must stay single roundings (no FMA).
 # Packed fp32 instructions are disabled for the device code.

@@ -1,0 +1,109 @@
+// Storing and loading byte checkpoints: streaming kernels, bound by memory (bf16: 3.02 B per value in either
+// direction with groups of 64; fp32: 5.02).
+//
+// A thread takes 16 consecutive columns of a row: 128-bit accesses on both sides, and the group's largest
+// magnitude needs two, four or eight neighbouring lanes (DPP, no LDS).  Rows are dealt to threads in units of whole
+// groups, so that a group never crosses a wave.
+#include "cmpz_byte.h"
+
+namespace cmpz {
+namespace {
+
+constexpr int kThreads = 256;
+
+template <uint32_t T, uint32_t F>
+__global__ __launch_bounds__(kThreads) void k_byte_store(ByteArgs a, uint64_t row0, uint32_t units, uint32_t steps,
+                                                         FastDiv div_units)
+{
+    typedef typename ElemOf<T>::type E;
+    const uint32_t at = blockIdx.x * kThreads + threadIdx.x;
+    const uint32_t r = div_units.div(at), c = (at - r * units) * 16u;
+    const uint64_t row = row0 + r;
+    const bool in = row < a.rows && c < a.cols;
+    const int n = in ? (int)(a.cols - c) : 0;                             // columns that exist from c on
+    const E *p = static_cast<const E *>(a.x) + (in ? row * a.ld + c : 0);
+    const f32x8 v0 = load8<T>(p, n), v1 = load8<T>(p + 8, n - 8);
+    const uint32_t e = group_exponent<F>(lanes_max(amax8(v1, amax8(v0, 0u)), steps));
+    if (blockIdx.x == 0 && row0 == 0 && threadIdx.x < a.tail_to - a.tail_from) a.codes[a.tail_from + threadIdx.x] = 0;
+    if (!in) return;
+    const float inv = inverse_scale_of(e);
+    const u32x2 lo = encode8<F>(v0, inv), hi = encode8<F>(v1, inv);       // columns that do not exist: zeros
+    u32x4 w = {lo[0], lo[1], hi[0], hi[1]};
+    *reinterpret_cast<u32x4 *>(a.codes + row * a.pitch + c) = w;
+    if ((c & ((1u << a.gshift) - 1u)) == 0) a.exps[row * a.ngroups + (c >> a.gshift)] = (uint8_t)e;
+}
+
+// Values beyond the output type's largest finite value (fp16 only: a code may round up past 65504) become that value.
+template <uint32_t T, uint32_t F>
+__global__ __launch_bounds__(kThreads) void k_byte_load(ByteArgs a, uint64_t row0, uint32_t units, FastDiv div_units)
+{
+    typedef typename ElemOf<T>::type E;
+    const uint32_t at = blockIdx.x * kThreads + threadIdx.x;
+    const uint32_t r = div_units.div(at), c = (at - r * units) * 16u;
+    const uint64_t row = row0 + r;
+    if (row >= a.rows) return;
+    const u32x4 w = *reinterpret_cast<const u32x4 *>(a.codes + row * a.pitch + c);
+    const float s = scale_of(a.exps[row * a.ngroups + (c >> a.gshift)]);
+    f32x8 v0 = decode8<F>(u32x2{w[0], w[1]}, s), v1 = decode8<F>(u32x2{w[2], w[3]}, s);
+    if constexpr (T == kTypeF16) {
+        auto held = [](float f) { return fabsf(f) > 65504.0f ? copysignf(65504.0f, f) : f; };   // NaN stays
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { v0[k] = held(v0[k]); v1[k] = held(v1[k]); }
+    }
+    const int n = (int)(a.cols - c);
+    E *p = static_cast<E *>(a.x) + row * a.ld + c;
+    store8<T>(p, v0, n);
+    store8<T>(p + 8, v1, n - 8);
+}
+
+// Launches over ranges of rows whose units can be counted with 31 bits.
+template <class LAUNCH>
+void by_rows(uint64_t rows, uint32_t units, LAUNCH go)
+{
+    const uint64_t most = (1ull << 31) / units;
+    for (uint64_t r = 0; r < rows; r += most) {
+        const uint64_t n = rows - r < most ? rows - r : most;
+        go(r, (uint32_t)((n * units + kThreads - 1) / kThreads));
+    }
+}
+
+template <uint32_t T, uint32_t F>
+void store_as(const ByteArgs &a, hipStream_t st)
+{
+    const uint32_t steps = a.gshift - 4, lanes = 1u << steps;
+    const uint32_t units = (uint32_t)((a.pitch / 16 + lanes - 1) / lanes * lanes);
+    const FastDiv d = FastDiv::make(units);
+    by_rows(a.rows, units, [&](uint64_t r, uint32_t grid) {
+        hipLaunchKernelGGL((k_byte_store<T, F>), dim3(grid), dim3(kThreads), 0, st, a, r, units, steps, d);
+    });
+}
+
+template <uint32_t T, uint32_t F>
+void load_as(const ByteArgs &a, hipStream_t st)
+{
+    const uint32_t units = (uint32_t)(a.pitch / 16);
+    const FastDiv d = FastDiv::make(units);
+    by_rows(a.rows, units, [&](uint64_t r, uint32_t grid) {
+        hipLaunchKernelGGL((k_byte_load<T, F>), dim3(grid), dim3(kThreads), 0, st, a, r, units, d);
+    });
+}
+
+}  // namespace
+
+void launch_byte_store(const ByteArgs &a, hipStream_t st)
+{
+    const bool i8 = a.format == kByteInt8;
+    if (a.type == kTypeF32) i8 ? store_as<kTypeF32, kByteInt8>(a, st) : store_as<kTypeF32, kByteE4M3>(a, st);
+    else if (a.type == kTypeF16) i8 ? store_as<kTypeF16, kByteInt8>(a, st) : store_as<kTypeF16, kByteE4M3>(a, st);
+    else i8 ? store_as<kTypeBF16, kByteInt8>(a, st) : store_as<kTypeBF16, kByteE4M3>(a, st);
+}
+
+void launch_byte_load(const ByteArgs &a, hipStream_t st)
+{
+    const bool i8 = a.format == kByteInt8;
+    if (a.type == kTypeF32) i8 ? load_as<kTypeF32, kByteInt8>(a, st) : load_as<kTypeF32, kByteE4M3>(a, st);
+    else if (a.type == kTypeF16) i8 ? load_as<kTypeF16, kByteInt8>(a, st) : load_as<kTypeF16, kByteE4M3>(a, st);
+    else i8 ? load_as<kTypeBF16, kByteInt8>(a, st) : load_as<kTypeBF16, kByteE4M3>(a, st);
+}
+
+}  // namespace cmpz
