@@ -152,8 +152,8 @@ int cmp_byte_linear_grad(int device, const cmp_byte_shape *shape, const void *d_
     LinearGradArgs a{};
     if (!shape_ok(shape) || outs > kMost || ld_dy < outs || type > CMP_TYPE_BF) return CMP_E_ARG;
     if (out_type != type && out_type != CMP_TYPE_F) return CMP_E_ARG;
-    const uint64_t tiles = ((outs + 127) / 128) * ((shape->cols + 127) / 128);
-    if (tiles > (1ull << 23)) return CMP_E_ARG;
+    // offsets within 32 rows are kept in 32 bits, workgroups counted by a launch
+    if (ld_dy > (1u << 24) || shape->cols > (1u << 24) || outs * shape->cols > (1ull << 36)) return CMP_E_ARG;
     const uint32_t es = type_bytes(type), os = type_bytes(out_type);
     if (shape->rows && outs && (!d_dy || misaligned(d_dy, es))) return CMP_E_ARG;
     if (shape->cols && outs && (!d_dw || misaligned(d_dw, os))) return CMP_E_ARG;

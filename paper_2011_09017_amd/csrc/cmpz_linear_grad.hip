@@ -6,14 +6,20 @@
 // or three bf16 terms that add up to the value exactly, at two or three times the matrix work.
 #include "cmpz_byte.h"
 
+#include <type_traits>
+
 namespace cmpz {
 namespace {
 
-typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float    f32x16 __attribute__((ext_vector_type(16)));
+typedef short    s16x4  __attribute__((ext_vector_type(4)));
+typedef __bf16   bf16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x4  __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
 
-constexpr int kTile = 128, kStep = 32, kThreads = 256;
-constexpr int kRow = kTile * 2 + 32;          // bytes of a row in LDS: four rows of a transposed read lie in different banks
+constexpr uint32_t kStep = 32;                 // rows of a stage: the reduction of one matrix instruction
+constexpr uint32_t kThreads = 256;             // four waves
+constexpr uint32_t kPad = 32;                  // behind a row in LDS: the four rows of a transposed read lie in different banks
 
 template <uint32_t T> constexpr int kTerms = T == kTypeBF16 ? 1 : T == kTypeF16 ? 2 : 3;
 
@@ -23,17 +29,22 @@ __device__ __forceinline__ uint32_t high_halves(float a, float b)
     return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
 
-// Sixteen codes as bf16.
+// Sixteen codes as bf16, at a quarter of their value (`s`: a quarter of their scale), which keeps 128 * s finite.
+// int8: the code -128, which stands for NaN, comes out as -128 * s; `found` collects whether there was one.
+constexpr float kShrink = 0.25f;
 template <uint32_t F>
-__device__ __forceinline__ void expand16(u32x4 w, float s, u32x4 *lo, u32x4 *hi)
+__device__ __forceinline__ void expand16(u32x4 w, float s, u32x4 *lo, u32x4 *hi, uint32_t *found)
 {
+    const float m = -128.0f * s;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         uint32_t p0, p1;
         if constexpr (F == kByteInt8) {
-            const f32x4 v = decode4<kByteInt8>(w[q], s);
-            p0 = high_halves(v[0], v[1]);
-            p1 = high_halves(v[2], v[3]);
+            const uint32_t u = w[q] ^ 0x80808080u;                        // code + 128
+            *found |= (u - 0x01010101u) & ~u;                             // a byte of zero leaves its highest bit
+            // exact: (code + 128) * s - 128 * s
+            p0 = high_halves(__builtin_fmaf((float)(u & 0xffu), s, m), __builtin_fmaf((float)((u >> 8) & 0xffu), s, m));
+            p1 = high_halves(__builtin_fmaf((float)((u >> 16) & 0xffu), s, m), __builtin_fmaf((float)(u >> 24), s, m));
         } else {
             const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[q], s, false);
             const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[q], s, true);
@@ -70,10 +81,11 @@ __device__ __forceinline__ void split8(f32x8 v, u32x4 *out)
 // Eight reduction rows of a column, as a matrix operand: lane l holds column l % 16, rows 8 * (l / 16) .. + 7.
 // `at`: the lane's address of row 8 * (l / 16) + (l % 16) / 4, column 4 * (l % 4); a group of 16 lanes reads four rows of
 // sixteen columns, which arrive transposed.
+template <uint32_t PITCH>
 __device__ __forceinline__ bf16x8 transposed(const uint8_t *at)
 {
     const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 4 * kRow));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 4 * PITCH));
     bf16x8 r;
     __builtin_memcpy(&r, &a, 8);
     __builtin_memcpy(reinterpret_cast<char *>(&r) + 8, &b, 8);
@@ -94,138 +106,416 @@ __device__ __forceinline__ void put(void *p, uint64_t i, uint32_t type, float v,
     }
 }
 
-struct Plan { uint32_t tiles_n, tiles_k, splits, rows_per; };
-
-template <uint32_t T, uint32_t F>
-__global__ __launch_bounds__(kThreads) void k_linear_grad(LinearGradArgs a, Plan p)
+// Four neighbouring results, of which `left` exist.
+__device__ __forceinline__ void put4(void *p, uint64_t i, uint32_t type, f32x4 v, uint32_t accumulate, int left)
 {
-    typedef typename ElemOf<T>::type E;
+    if (left == 4 && !accumulate) {
+        if (type == kTypeF32) {
+            __builtin_memcpy(static_cast<float *>(p) + i, &v, 16);
+        } else if (type == kTypeF16) {
+            const f16x4 h = __builtin_convertvector(v, f16x4);
+            __builtin_memcpy(static_cast<_Float16 *>(p) + i, &h, 8);
+        } else {
+            const bf16x4 h = __builtin_convertvector(v, bf16x4);
+            __builtin_memcpy(static_cast<__bf16 *>(p) + i, &h, 8);
+        }
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (k < left) put(p, i + k, type, v[k], accumulate);
+}
+
+struct Plan { uint32_t tiles_n, tiles_k, splits, rows_per, parts_b; };     // parts_b: partial sums of db
+
+// Eight values of dY as they lie in memory.
+template <uint32_t T> struct Raw { u32x4 w[T == kTypeF32 ? 2 : 1]; };
+template <uint32_t T>
+__device__ __forceinline__ f32x8 values_of(const Raw<T> &r)
+{
+    f32x8 v;
+    if constexpr (T == kTypeF32) {
+        __builtin_memcpy(&v, &r, 32);
+    } else if constexpr (T == kTypeF16) {
+        f16x8 h;
+        __builtin_memcpy(&h, &r, 16);
+        v = __builtin_convertvector(h, f32x8);
+    } else {
+        bf16x8 h;
+        __builtin_memcpy(&h, &r, 16);
+        v = __builtin_convertvector(h, f32x8);
+    }
+    return v;
+}
+
+// A workgroup computes TN x TK results over a range of rows, 32 rows (a stage) at a time.  Four waves, WN x WK of them, take
+// FN x FK results of 32 x 32 each.  Two stages lie in LDS.  While the matrix units work on the operands of stage t, which
+// are in registers, a wave reads those of stage t + 1, stores stage t + 2 over stage t (which every wave has read
+// when it passes the one barrier of the stage) and loads stage t + 4 from memory.  The number of stages is even, so that
+// registers and LDS slots alternate by a compile-time index; rows of zeros before the first fill the first two.
+template <uint32_t T, uint32_t F, int FN, int FK, int WN, int WK>
+__global__ __launch_bounds__(kThreads, FN * FK > 4 ? 1 : 2) void k_linear_grad(LinearGradArgs a, Plan p)
+{
     constexpr int TERMS = kTerms<T>;
-    __shared__ __align__(16) uint8_t s_y[TERMS][kStep * kRow];
-    __shared__ __align__(16) uint8_t s_x[kStep * kRow];
+    constexpr uint32_t ES = type_bytes(T);
+    constexpr uint32_t TN = FN * 32 * WN, TK = FK * 32 * WK;
+    constexpr uint32_t PY = TN * 2 + kPad, PX = TK * 2 + kPad;            // bytes of a row in LDS
+    constexpr uint32_t VY = TN / 8, VX = TK / 16;                         // vectors of a row
+    constexpr uint32_t YV = VY * kStep / kThreads, XV = VX * kStep >= kThreads ? VX * kStep / kThreads : 1;
+    constexpr uint32_t RY = kThreads / VY, RX = kThreads / VX;            // rows between a thread's vectors
+    static_assert(WN * WK == 4 && YV >= 1, "four waves");
+    // one block of LDS: two stages of dY's terms, two of x', and at the end the rows of the results
+    constexpr uint32_t SY = kStep * PY, SX = kStep * PX, RW = FK * 32 + 4, RV = FK * 8;
+    constexpr uint32_t kStages = 2 * TERMS * SY + 2 * SX, kRows = 4 * 32 * RW * 4;
+    __shared__ __align__(16) uint8_t s_all[kStages > kRows ? kStages : kRows];
+    auto s_y = [&](int slot, int term) -> uint8_t * { return s_all + (slot * TERMS + term) * SY; };
+    auto s_x = [&](int slot) -> uint8_t * { return s_all + 2 * TERMS * SY + slot * SX; };
+
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
     uint32_t b = blockIdx.x;
     const uint32_t tn = b % p.tiles_n; b /= p.tiles_n;
     const uint32_t tk = b % p.tiles_k, split = b / p.tiles_k;
-    const uint32_t n0 = tn * kTile, k0 = tk * kTile;
+    const uint32_t n_first = tn * TN, k0 = tk * TK;
+    // a last tile of fewer than eight columns starts earlier, so that a vector of its columns fits (they are stored once)
+    const uint32_t n0 = a.outs - n_first < 8 ? a.outs - 8 : n_first;
     const uint32_t m_beg = split * p.rows_per;
     const uint32_t m_end = a.rows - m_beg < p.rows_per ? a.rows : m_beg + p.rows_per;
-    const bool with_db = a.db && tk == 0;
+    const uint32_t stages = ((m_end - m_beg + kStep - 1) / kStep + 1) & ~1u;
+    const int64_t m_zero = (int64_t)m_end - (int64_t)stages * kStep;      // first row of stage 0: m_beg, or up to 63 before it
 
-    f32x4 acc[4][4], accb[4];
+    // ---- what this thread brings from memory: YV vectors of dY and XV of codes ----
+    const uint32_t ry = tid / VY, cy = (tid % VY) * 8u;
+    // the vector that crosses the last column moves back into the row, here and in LDS; those behind it, and codes
+    // behind the last column, read anything: their results are not stored
+    const uint32_t ny = n0 + cy + 8 > a.outs ? a.outs - 8 : n0 + cy;
+    const uint32_t dst_y = n0 + cy < a.outs ? ny - n0 : cy;
+    const uint32_t rx = (tid / VX) & (kStep - 1u), cx = (tid % VX) * 16u; // (small tiles: several threads bring the same codes)
+    const uint32_t kx = k0 + cx < a.cols ? k0 + cx : (uint32_t)a.pitch - 16u;
+    const uint8_t *dy = static_cast<const uint8_t *>(a.dy);
+    const uint64_t row_y = a.ld_dy * ES;
+    // offsets from the first row of a stage: rows are at most 2^24 values apart
+    uint32_t off_y[YV], off_x[XV], off_e[XV];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        accb[i] = f32x4{0, 0, 0, 0};
+    for (uint32_t q = 0; q < YV; ++q) off_y[q] = (ry + q * RY) * (uint32_t)row_y + ny * ES;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+    for (uint32_t q = 0; q < XV; ++q) {
+        off_x[q] = (rx + q * RX) * (uint32_t)a.pitch + kx;
+        off_e[q] = (rx + q * RX) * (uint32_t)a.ngroups + (kx >> a.gshift);
     }
-    const uint32_t wk = (wave & 1u) * 64u, wn = (wave >> 1) * 64u;
-    const uint32_t frag = ((lane >> 4) * 8u + ((lane & 15u) >> 2)) * kRow + (lane & 3u) * 8u;
-    bf16x8 ones;
+    struct Fetched { Raw<T> y[YV]; u32x4 x[XV]; uint32_t e[XV]; } got[2];
+    auto load = [&](Fetched &g, uint32_t s) {                             // stage 2 or later: all its rows exist
+        if (s >= stages) return;
+        const uint64_t m0 = (uint64_t)(m_zero + (int64_t)s * kStep);
+        const uint8_t *y = dy + m0 * row_y, *x = a.codes + m0 * a.pitch, *e = a.exps + m0 * a.ngroups;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) ones[k] = (__bf16)1.0f;
-
-    for (uint32_t m0 = m_beg; m0 < m_end; m0 += kStep) {
-        // dY: rows of 16 vectors of eight; codes: rows of eight times sixteen
+        for (uint32_t q = 0; q < YV; ++q) __builtin_memcpy(&g.y[q], y + off_y[q], sizeof(g.y[q]));
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const uint32_t r = (tid >> 4) + 16u * q, c = (tid & 15u) * 8u, m = m0 + r;
-            const int n = m < m_end && n0 + c < a.outs ? (int)(a.outs - n0 - c) : 0;
-            const E *src = static_cast<const E *>(a.dy) + (n > 0 ? (uint64_t)m * a.ld_dy + n0 + c : 0);
-            u32x4 t[TERMS];
-            split8<T>(load8<T>(src, n), t);
-#pragma unroll
-            for (int k = 0; k < TERMS; ++k) *reinterpret_cast<u32x4 *>(&s_y[k][r * kRow + c * 2u]) = t[k];
+        for (uint32_t q = 0; q < XV; ++q) {
+            g.x[q] = *reinterpret_cast<const u32x4 *>(x + off_x[q]);
+            g.e[q] = e[off_e[q]];
         }
-        {
-            const uint32_t r = tid >> 3, c = (tid & 7u) * 16u, m = m0 + r;
-            u32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
-            if (m < m_end && k0 + c < a.cols) {
-                const u32x4 w = *reinterpret_cast<const u32x4 *>(a.codes + (uint64_t)m * a.pitch + k0 + c);
-                expand16<F>(w, scale_of(a.exps[(uint64_t)m * a.ngroups + ((k0 + c) >> a.gshift)]), &lo, &hi);
+    };
+    auto load_first = [&](Fetched &g, uint32_t s) {                       // stage 0 or 1: rows before m_beg are zero in both operands
+        const int64_t m0 = m_zero + (int64_t)s * kStep;
+#pragma unroll
+        for (uint32_t q = 0; q < YV; ++q) {
+            const int64_t m = m0 + ry + q * RY;
+            g.y[q] = Raw<T>{};
+            if (m >= (int64_t)m_beg) __builtin_memcpy(&g.y[q], dy + (uint64_t)m * row_y + (uint64_t)ny * ES, sizeof(g.y[q]));
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < XV; ++q) {
+            const int64_t m = m0 + rx + q * RX;
+            g.x[q] = u32x4{0, 0, 0, 0};
+            g.e[q] = 127;
+            if (m >= (int64_t)m_beg) {
+                g.x[q] = *reinterpret_cast<const u32x4 *>(a.codes + (uint64_t)m * a.pitch + kx);
+                g.e[q] = a.exps[(uint64_t)m * a.ngroups + (kx >> a.gshift)];
             }
-            *reinterpret_cast<u32x4 *>(&s_x[r * kRow + c * 2u]) = lo;
-            *reinterpret_cast<u32x4 *>(&s_x[r * kRow + c * 2u + 16u]) = hi;
+        }
+    };
+    // into LDS; returns a word with one of the bits 0x80808080 set where a code stands for NaN
+    auto store = [&](const Fetched &g, int slot) -> uint32_t {
+#pragma unroll
+        for (uint32_t q = 0; q < YV; ++q) {
+            const uint32_t at = (ry + q * RY) * PY + dst_y * 2u;
+            if constexpr (T == kTypeBF16) {
+                *reinterpret_cast<u32x4 *>(s_y(slot, 0) + at) = g.y[q].w[0];
+            } else {
+                u32x4 t[TERMS];
+                split8<T>(values_of<T>(g.y[q]), t);
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) *reinterpret_cast<u32x4 *>(s_y(slot, k) + at) = t[k];
+            }
+        }
+        uint32_t found = 0;
+#pragma unroll
+        for (uint32_t q = 0; q < XV; ++q) {
+            u32x4 lo, hi;
+            expand16<F>(g.x[q], scale_of(g.e[q]) * kShrink, &lo, &hi, &found);
+            uint8_t *at = s_x(slot) + (rx + q * RX) * PX + cx * 2u;
+            *reinterpret_cast<u32x4 *>(at) = lo;
+            *reinterpret_cast<u32x4 *>(at + 16) = hi;
+        }
+        return found;
+    };
+    auto mark_nan = [&](const Fetched &g, int slot) {
+#pragma unroll 1
+        for (uint32_t k = 0; k < 16u * XV; ++k) {
+            const uint32_t q = k >> 4, c = k & 15u;
+            uint32_t w = 0;
+#pragma unroll
+            for (uint32_t i = 0; i < XV; ++i)
+#pragma unroll
+                for (uint32_t h = 0; h < 4; ++h)
+                    if (i == q && h == c >> 2) w = g.x[i][h];
+            if (((w >> (8u * (c & 3u))) & 0xffu) == 0x80u)
+                *reinterpret_cast<uint16_t *>(s_x(slot) + (rx + q * RX) * PX + (cx + c) * 2u) = 0x7fc0u;
+        }
+    };
+    // the bias gradient's share of this workgroup: every tiles_k-th stage
+    float sum_b[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum_b[k] = 0.0f;
+    uint32_t next_b = a.db ? tk : 0xffffffffu;
+    auto sum_bias = [&](const Fetched &g, uint32_t s) {
+        if (s != next_b || s >= stages) return;
+        next_b += p.tiles_k;
+#pragma unroll
+        for (uint32_t q = 0; q < YV; ++q) {
+            const f32x8 v = values_of<T>(g.y[q]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum_b[k] += v[k];
+        }
+    };
+
+    // ---- operands and results of this wave ----
+    const uint32_t wk = (wave % WK) * (FK * 32u), wn = (wave / WK) * (FN * 32u);
+    const uint32_t frag_row = (lane >> 5) * 8u + ((lane & 15u) >> 2), frag_col = ((lane >> 4) & 1u) * 32u + (lane & 3u) * 8u;
+    const uint32_t at_y = frag_row * PY + frag_col + wn * 2u, at_x = frag_row * PX + frag_col + wk * 2u;
+    f32x16 acc[FK][FN];
+#pragma unroll
+    for (int i = 0; i < FK; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = f32x16{};
+    bf16x8 fy[2][2][FN], fx[2][2][FK];                                    // [buffer][half of the stage]
+    auto read_y = [&](bf16x8 (&f)[2][FN], int slot, int term) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) f[h][j] = transposed<PY>(s_y(slot, term) + at_y + h * 16u * PY + 64u * j);
+    };
+    auto read_x = [&](bf16x8 (&f)[2][FK], int slot) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < FK; ++i) f[h][i] = transposed<PX>(s_x(slot) + at_x + h * 16u * PX + 64u * i);
+    };
+    auto multiply = [&](const bf16x8 (&x)[FK], const bf16x8 (&y)[FN]) {
+#pragma unroll
+        for (int i = 0; i < FK; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
+    };
+
+    auto step = [&](auto parity, uint32_t t) {
+        constexpr int P = decltype(parity)::value;
+#pragma unroll
+        for (int u = 0; u + 1 < TERMS; ++u) {
+            const int now = (P * TERMS + u) & 1;
+            read_y(fy[now ^ 1], P, u + 1);
+            multiply(fx[P][0], fy[now][0]);
+            multiply(fx[P][1], fy[now][1]);
+        }
+        constexpr int now = (P * TERMS + TERMS - 1) & 1;
+        // every wave has the last operands of stage t in registers, and stage t + 1 is stored
+        __syncthreads();
+        read_y(fy[now ^ 1], P ^ 1, 0);
+        read_x(fx[P ^ 1], P ^ 1);
+        multiply(fx[P][0], fy[now][0]);
+        // reads between the first half's products, the expansion and its stores between the second half's
+#pragma unroll
+        for (int k = 0; k < FN * FK; ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);            // matrix
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);            // LDS reads
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const uint32_t found = store(got[P], P);
+        multiply(fx[P][1], fy[now][1]);
+#pragma unroll
+        for (int k = 0; k < FN * FK; ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(0x002, 6, 1);            // vector arithmetic
+            if (k & 1) __builtin_amdgcn_sched_group_barrier(0x200, 1, 1); // LDS writes
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (F == kByteInt8 && (found & 0x80808080u)) mark_nan(got[P], P);
+        sum_bias(got[P], t + 2);
+        load(got[P], t + 4);
+    };
+
+    if (stages > 0) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            load_first(got[s], s);
+            if (store(got[s], s) & 0x80808080u) mark_nan(got[s], s);
+            sum_bias(got[s], s);
+            load(got[s], s + 2);
         }
         __syncthreads();
-        bf16x8 fx[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) fx[i] = transposed(s_x + frag + (wk + 16u * i) * 2u);
-#pragma unroll
-        for (int t = 0; t < TERMS; ++t) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bf16x8 fy = transposed(s_y[t] + frag + (wn + 16u * j) * 2u);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[i], fy, acc[i][j], 0, 0, 0);
-                if (with_db) accb[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fy, accb[j], 0, 0, 0);
-            }
-        }
-        __syncthreads();
+        read_y(fy[0], 0, 0);
+        read_x(fx[0], 0);
+    }
+#pragma unroll 1
+    for (uint32_t t = 0; t < stages; t += 2) {
+        step(std::integral_constant<int, 0>{}, t);
+        step(std::integral_constant<int, 1>{}, t + 1);
     }
 
-    // lane: output row n = lane % 16, four consecutive k
-    float *part = p.splits > 1 ? a.work + (uint64_t)split * a.outs * a.cols : nullptr;
-    float *part_b = p.splits > 1 ? a.work + (uint64_t)p.splits * a.outs * a.cols + (uint64_t)split * a.outs : nullptr;
+    // ---- results: a lane holds column n = lane % 16 and four consecutive k of every 16 x 16; sixteen rows of dW at a
+    // time go through LDS, so that a row is stored by neighbouring lanes ----
+    __syncthreads();
+    float *rows = reinterpret_cast<float *>(s_all) + wave * (32u * RW);   // RW floats a row, RV vectors of four in it
+    void *out = p.splits > 1 ? static_cast<void *>(a.work + (uint64_t)split * a.outs * a.cols) : a.dw;
+    const uint32_t out_type = p.splits > 1 ? kTypeF32 : a.out_type, accumulate = p.splits > 1 ? 0u : a.accumulate;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t n = n0 + wn + 16u * j + (lane & 15u);
-        if (n >= a.outs) continue;
+    for (int j = 0; j < FN; ++j) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t k = k0 + wk + 16u * i + (lane >> 4) * 4u;
+        for (int i = 0; i < FK; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (k + q >= a.cols) continue;
-                if (part) part[(uint64_t)n * a.cols + k + q] = acc[i][j][q];
-                else put(a.dw, (uint64_t)n * a.cols + k + q, a.out_type, acc[i][j][q], a.accumulate);
-            }
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<f32x4 *>(rows + (lane & 31u) * RW + 32u * i + 8u * q + (lane >> 5) * 4u) =
+                    f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]} * (1.0f / kShrink);
+        const uint32_t n_row = n0 + wn + 32u * j;
+#pragma unroll 1
+        for (uint32_t v = lane; v < 32u * RV; v += 64u) {
+            const uint32_t r = v / RV, c = (v % RV) * 4u, n = n_row + r, k = k0 + wk + c;
+            if (n >= n_first && n < a.outs && k < a.cols)
+                put4(out, (uint64_t)n * a.cols + k, out_type, *reinterpret_cast<const f32x4 *>(rows + r * RW + c), accumulate,
+                     a.cols - k < 4 ? (int)(a.cols - k) : 4);
         }
-        if (with_db && wk == 0 && lane < 16u) {
-            if (part) part_b[n] = accb[j][0];
-            else put(a.db, n, a.out_type, accb[j][0], a.accumulate);
+    }
+    if (a.db) {                                                           // columns of the threads with the same vector
+        float *s = reinterpret_cast<float *>(s_all);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[tid * 8u + k] = sum_b[k];
+        __syncthreads();
+        float *part_b = a.work + (p.splits > 1 ? (uint64_t)p.splits * a.outs * a.cols : 0) + (uint64_t)(split * p.tiles_k + tk) * a.outs;
+        if (tid < VY && n0 + cy < a.outs) {
+            for (int k = 0; k < 8 && ny + k < a.outs; ++k) {
+                if (ny + k < n_first || ny + k < n0 + cy) continue;      // a vector moved back shares columns with the one before it
+                float v = 0.0f;
+                for (uint32_t r = 0; r < kThreads / VY; ++r) v += s[(r * VY + tid) * 8u + k];
+                if (p.parts_b > 1) part_b[ny + k] = v;
+                else put(a.db, ny + k, a.out_type, v, a.accumulate);
+            }
         }
     }
 }
 
-// Joins the partial sums of the ranges of rows, in their order.
-__global__ __launch_bounds__(kThreads) void k_linear_grad_join(LinearGradArgs a, uint32_t splits, uint64_t values)
+// Fewer than eight outputs (a gate, a small head), or no columns at all: too narrow for the matrix tiles.  A thread takes
+// four columns and eight outputs over a range of rows, in fp32; bound by reading the codes once.
+template <uint32_t T, uint32_t F>
+__global__ __launch_bounds__(kThreads) void k_linear_grad_few(LinearGradArgs a, Plan p)
+{
+    typedef typename ElemOf<T>::type E;
+    uint32_t b = blockIdx.x;
+    const uint32_t tn = b % p.tiles_n; b /= p.tiles_n;
+    const uint32_t tk = b % p.tiles_k, split = b / p.tiles_k;
+    const uint32_t n0 = tn * 8u, k0 = (tk * kThreads + threadIdx.x) * 4u;
+    const uint32_t m_beg = split * p.rows_per, m_end = a.rows - m_beg < p.rows_per ? a.rows : m_beg + p.rows_per;
+    const int n = (int)(a.outs - n0);
+    const bool mine = k0 < a.cols, with_db = a.db && tk == 0 && threadIdx.x == 0;
+    f32x4 acc[8];
+    f32x8 sum = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = f32x4{0, 0, 0, 0};
+    if (mine || with_db) {
+        const E *dy = static_cast<const E *>(a.dy) + n0;
+#pragma unroll 4
+        for (uint32_t m = m_beg; m < m_end; ++m) {
+            const f32x8 y = load8<T>(dy + (uint64_t)m * a.ld_dy, n);
+            sum += y;
+            if (mine) {
+                const f32x4 x = decode4<F>(*reinterpret_cast<const uint32_t *>(a.codes + (uint64_t)m * a.pitch + k0),
+                                           scale_of(a.exps[(uint64_t)m * a.ngroups + (k0 >> a.gshift)]));
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[j][q] = __builtin_fmaf(y[j], x[q], acc[j][q]);
+            }
+        }
+    }
+    void *out = p.splits > 1 ? static_cast<void *>(a.work + (uint64_t)split * a.outs * a.cols) : a.dw;
+    float *part_b = a.work + (uint64_t)p.splits * a.outs * a.cols + (uint64_t)split * a.outs;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if (j >= n) continue;
+        if (mine)
+            put4(out, (uint64_t)(n0 + j) * a.cols + k0, p.splits > 1 ? kTypeF32 : a.out_type, acc[j], p.splits > 1 ? 0u : a.accumulate,
+                 a.cols - k0 < 4 ? (int)(a.cols - k0) : 4);
+        if (with_db) {
+            if (p.splits > 1) part_b[n0 + j] = sum[j];
+            else put(a.db, n0 + j, a.out_type, sum[j], a.accumulate);
+        }
+    }
+}
+
+// Joins the partial sums of the ranges of rows, in their order; dW's if there are several, db's.
+__global__ __launch_bounds__(kThreads) void k_linear_grad_join(LinearGradArgs a, uint32_t splits, uint32_t splits_b, uint64_t values)
 {
     const uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i < values) {
+    const uint64_t first = splits > 1 ? values : 0;                       // work items of dW, before those of db
+    if (i < first) {
         float s = 0.0f;
         for (uint32_t k = 0; k < splits; ++k) s += a.work[(uint64_t)k * values + i];
         put(a.dw, i, a.out_type, s, a.accumulate);
-    } else if (a.db && i - values < a.outs) {
+    } else if (a.db && splits_b > 1 && i - first < a.outs) {
+        const float *w = a.work + (uint64_t)(splits > 1 ? splits : 0) * values + (i - first);
         float s = 0.0f;
-        for (uint32_t k = 0; k < splits; ++k) s += a.work[(uint64_t)splits * values + (uint64_t)k * a.outs + (i - values)];
-        put(a.db, i - values, a.out_type, s, a.accumulate);
+        for (uint32_t k = 0; k < splits_b; ++k) s += w[(uint64_t)k * a.outs];
+        put(a.db, i - first, a.out_type, s, a.accumulate);
     }
 }
+
+constexpr uint32_t kTileN = 256, kTileK = 256;
+
+bool few_outputs(uint64_t cols, uint64_t outs) { return outs < 8 || cols == 0; }
 
 Plan make_plan(uint64_t rows, uint64_t cols, uint64_t outs)
 {
     Plan p;
-    p.tiles_n = outs ? (uint32_t)((outs + kTile - 1) / kTile) : 1;
-    p.tiles_k = cols ? (uint32_t)((cols + kTile - 1) / kTile) : 1;         // without columns the bias gradient is left
-    const uint64_t tiles = (uint64_t)p.tiles_n * p.tiles_k;
-    uint64_t splits = tiles >= 512 ? 1 : 512 / tiles;
-    const uint64_t steps = (rows + kStep - 1) / kStep;
-    if (splits > (steps + 7) / 8) splits = (steps + 7) / 8;                // no fewer than eight steps each
+    const bool few = few_outputs(cols, outs);
+    const uint32_t tile_n = few ? 8 : kTileN, tile_k = few ? 4 * kThreads : kTileK;
+    p.tiles_n = outs ? (uint32_t)((outs + tile_n - 1) / tile_n) : 1;
+    p.tiles_k = cols ? (uint32_t)((cols + tile_k - 1) / tile_k) : 1;       // without columns the bias gradient is left
+    const uint64_t tiles = (uint64_t)p.tiles_n * p.tiles_k, want = few ? 1024 : 256;
+    uint64_t splits = tiles >= want ? 1 : want / tiles;
+    const uint64_t steps = (rows + kStep - 1) / kStep, least = few ? 2 : 8;
+    if (splits > (steps + least - 1) / least) splits = (steps + least - 1) / least;
     if (splits < 1) splits = 1;
     p.rows_per = (uint32_t)((steps + splits - 1) / splits * kStep);
     if (p.rows_per == 0) p.rows_per = kStep;
     p.splits = (uint32_t)((rows + p.rows_per - 1) / p.rows_per);
     if (p.splits < 1) p.splits = 1;
+    p.parts_b = few ? p.splits : p.splits * p.tiles_k;
     return p;
 }
 
-template <uint32_t T>
+template <uint32_t T, uint32_t F>
 void launch_as(const LinearGradArgs &a, const Plan &p, hipStream_t st)
 {
-    const dim3 grid(p.tiles_n * p.tiles_k * p.splits);
-    if (a.format == kByteInt8) hipLaunchKernelGGL((k_linear_grad<T, kByteInt8>), grid, dim3(kThreads), 0, st, a, p);
-    else hipLaunchKernelGGL((k_linear_grad<T, kByteE4M3>), grid, dim3(kThreads), 0, st, a, p);
+    const dim3 grid(p.tiles_n * p.tiles_k * p.splits), block(kThreads);
+    if (few_outputs(a.cols, a.outs)) hipLaunchKernelGGL((k_linear_grad_few<T, F>), grid, block, 0, st, a, p);
+    else hipLaunchKernelGGL((k_linear_grad<T, F, 4, 4, 2, 2>), grid, block, 0, st, a, p);
+}
+
+template <uint32_t T>
+void launch_of(const LinearGradArgs &a, const Plan &p, hipStream_t st)
+{
+    if (a.format == kByteInt8) launch_as<T, kByteInt8>(a, p, st);
+    else launch_as<T, kByteE4M3>(a, p, st);
 }
 
 }  // namespace
@@ -233,20 +523,20 @@ void launch_as(const LinearGradArgs &a, const Plan &p, hipStream_t st)
 uint64_t linear_grad_work(uint64_t rows, uint64_t cols, uint64_t outs, uint32_t type)
 {
     const Plan p = make_plan(rows, cols, outs);
-    return p.splits > 1 ? 4ull * p.splits * (outs * cols + outs) : 0;
+    return 4ull * ((p.splits > 1 ? p.splits * outs * cols : 0) + (p.parts_b > 1 ? p.parts_b * outs : 0));
 }
 
 void launch_linear_grad(const LinearGradArgs &a, hipStream_t st)
 {
     const Plan p = make_plan(a.rows, a.cols, a.outs);
-    if (a.type == kTypeF32) launch_as<kTypeF32>(a, p, st);
-    else if (a.type == kTypeF16) launch_as<kTypeF16>(a, p, st);
-    else launch_as<kTypeBF16>(a, p, st);
-    if (p.splits > 1) {
-        const uint64_t values = (uint64_t)a.outs * a.cols;
-        hipLaunchKernelGGL(k_linear_grad_join, dim3((uint32_t)((values + a.outs + kThreads - 1) / kThreads)), dim3(kThreads),
-                           0, st, a, p.splits, values);
-    }
+    if (a.type == kTypeF32) launch_of<kTypeF32>(a, p, st);
+    else if (a.type == kTypeF16) launch_of<kTypeF16>(a, p, st);
+    else launch_of<kTypeBF16>(a, p, st);
+    const uint64_t values = (uint64_t)a.outs * a.cols;
+    const uint64_t items = (p.splits > 1 ? values : 0) + (a.db && p.parts_b > 1 ? a.outs : 0);
+    if (items)
+        hipLaunchKernelGGL(k_linear_grad_join, dim3((uint32_t)((items + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, a, p.splits,
+                           p.parts_b, values);
 }
 
 }  // namespace cmpz

@@ -26,7 +26,7 @@ def test_library_refusals():
         return b.cmp_byte_linear_grad(0, s, a["ck"], a["bytes"], a["dy"], a["type"], a["outs"], a["ld"], a["dw"], a["db"], a["out"],
                                       False, a["work"], a["need"], 0)
     for kw in (dict(ck=0), dict(ck=P + 4), dict(dy=0), dict(dy=P + 1), dict(type=3), dict(outs=1 << 31), dict(ld=23), dict(dw=0),
-               dict(dw=P + 1), dict(db=P + 1), dict(out=1), dict(out=3), dict(outs=(1 << 30) + 128, ld=1 << 31)):
+               dict(dw=P + 1), dict(db=P + 1), dict(out=1), dict(out=3), dict(ld=(1 << 24) + 1)):
         assert call(**kw) == b.CMP_E_ARG, kw
     assert call(bytes=n - 1) == b.CMP_E_FORMAT
     for rows, cols, outs in ((0, 0, 0), (5, 0, 3), (5, 3, 0), (0, 3, 3), (1, 1, 1)):
