@@ -6,33 +6,49 @@
 //             du = dy * act'(u);  dbeta = sum du, dgamma = sum du * h over batch and positions;
 //             A = sum du * gamma, B = sum du * gamma * h over a group;  dx = r * (du * gamma - (A + h * B) / count)
 //
-// Two passes each: the sums need all of a sample before the first output.  A workgroup takes a range of positions
-// with all their channels, a thread eight neighbouring channels (128-bit accesses whatever a group's width is) of
-// every rp-th position; sums are kept per channel and thread and joined per channel, then per group, in LDS.
+// The sums need all of a sample before the first output.  Where a sample's channels can be cut into segments of whole
+// groups that fit the registers of one workgroup, that workgroup reads its segment once and does everything (k_norm_slab,
+// k_norm_grad_slab).  Otherwise there are two passes: a workgroup takes a range of positions with all their channels.
+// In both a thread takes eight neighbouring channels (128-bit accesses whatever a group's width is) of every rp-th
+// position; sums are kept per channel and thread and joined per channel, then per group, in LDS.
 #include "cmpz_byte.h"
+
+#include <type_traits>
 
 namespace cmpz {
 namespace {
 
 constexpr uint32_t kMaxThreads = 1024;
 constexpr uint32_t kPlain = 2;                 // source of the input: not codes
+constexpr uint32_t kSlabRows = 4;              // positions that a thread of a slab keeps in registers
 
 struct Plan {
-    uint32_t nv;          // threads of a position: vectors of eight channels, in whole quantisation groups
+    uint32_t nv;          // threads of a position: vectors of eight channels (two passes: in whole quantisation groups)
     uint32_t rp;          // positions side by side
     uint32_t threads;
-    uint32_t chunks;      // workgroups of a sample
+    uint32_t chunks;      // workgroups of a sample: ranges of positions, or segments of channels
     uint32_t rows_per;    // positions of a workgroup
+    uint32_t per;         // channels of a group
+    double   share;       // 1 / (positions * per)
     FastDiv  div_nv, div_chunks, div_per;
 };
 
-Plan make_plan(const NormArgs &a, uint32_t lanes)
+void finish_plan(Plan *p, const NormArgs &a)
 {
-    Plan p;
+    p->threads = (p->nv * p->rp + 63) / 64 * 64;
+    p->per = a.channels / a.groups;
+    p->share = a.spatial ? 1.0 / ((double)a.spatial * (double)p->per) : 0.0;
+    p->div_nv = FastDiv::make(p->nv);
+    p->div_chunks = FastDiv::make(p->chunks);
+    p->div_per = FastDiv::make(p->per);
+}
+
+Plan two_pass_plan(const NormArgs &a, uint32_t lanes)
+{
+    Plan p{};
     p.nv = ((a.channels + 7) / 8 + lanes - 1) / lanes * lanes;
     p.rp = p.nv >= 512 ? 1 : 512 / p.nv;
     if (p.rp > a.spatial) p.rp = a.spatial ? a.spatial : 1;
-    p.threads = (p.nv * p.rp + 63) / 64 * 64;
     const uint64_t want = a.batch ? (1024 + a.batch - 1) / a.batch : 1;
     uint64_t chunks = (a.spatial + p.rp * 4ull - 1) / (p.rp * 4ull);
     if (chunks > want) chunks = want;
@@ -41,10 +57,45 @@ Plan make_plan(const NormArgs &a, uint32_t lanes)
     if (p.rows_per < 1) p.rows_per = 1;
     p.chunks = (a.spatial + p.rows_per - 1) / p.rows_per;
     if (p.chunks < 1) p.chunks = 1;
-    p.div_nv = FastDiv::make(p.nv);
-    p.div_chunks = FastDiv::make(p.chunks);
-    p.div_per = FastDiv::make(a.channels / a.groups);
+    finish_plan(&p, a);
     return p;
+}
+
+uint32_t lcm(uint32_t x, uint32_t y)
+{
+    uint32_t g = x, h = y;
+    while (h) { const uint32_t t = g % h; g = h; h = t; }
+    return x / g * y;
+}
+
+// The smallest segment is a multiple of eight channels, of a group and, where codes are written, of a quantisation group
+// (or all channels).  It grows to 128 bytes of a position as long as it fits.  Small segments, down to a single wave, keep
+// all of a CU's registers busy with loads.
+bool slab_plan(Plan *out, const NormArgs &a, uint32_t lanes)
+{
+    if (a.spatial == 0) return false;
+    Plan p{};
+    const uint32_t all = (a.channels + 7) / 8;
+    uint32_t unit = lcm(8u * lanes, a.channels / a.groups) / 8;
+    if (unit >= all) unit = (all + lanes - 1) / lanes * lanes;
+    const uint64_t most = (uint64_t)kMaxThreads * kSlabRows;
+    auto fits = [&](uint32_t nv) { return (uint64_t)nv * a.spatial <= most && nv <= kMaxThreads; };
+    if (!fits(unit)) return false;
+    p.nv = unit;
+    while (p.nv + unit <= all && fits(p.nv + unit) && p.nv * 8 * type_bytes(a.type) < 128) p.nv += unit;
+    p.chunks = (all + p.nv - 1) / p.nv;
+    // Positions per thread: as many as it can hold, so that a CU has most bytes in flight; one where all threads fit the
+    // chip at once and only the time of a single workgroup counts.
+    const uint64_t vectors = (uint64_t)p.nv * a.spatial;
+    uint32_t rows = (uint32_t)((vectors + kMaxThreads - 1) / kMaxThreads);
+    if (a.batch * p.chunks * vectors > 256ull * kMaxThreads && rows < kSlabRows) rows = kSlabRows;
+    p.rp = (a.spatial + rows - 1) / rows;
+    while ((uint64_t)p.rp * p.nv > kMaxThreads) p.rp = (a.spatial + ++rows - 1) / rows;
+    if (rows > kSlabRows) return false;
+    p.rows_per = a.spatial;
+    finish_plan(&p, a);
+    *out = p;
+    return true;
 }
 
 __device__ __forceinline__ double wave_sum(double v)
@@ -59,40 +110,47 @@ __device__ __forceinline__ float sigmoid(float u)
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * u));
 }
 
-// The place of a thread: its vector of eight channels and its first position, and those of its workgroup.
-struct Place { uint32_t n, chunk, v, r, row_beg, row_end; int valid; };
-__device__ __forceinline__ Place place(const NormArgs &a, const Plan &p, uint32_t block)
+__device__ __forceinline__ float activate(float u, uint32_t act)
+{
+    return act == kActSilu ? u * sigmoid(u) : act == kActRelu ? (u > 0.0f ? u : u != u ? u : 0.0f) : u;
+}
+
+// The place of a thread: its sample, its first channel, how many of its eight channels exist, its first position.
+struct Place { uint32_t n, chunk, c, v, r; int valid; };
+__device__ __forceinline__ Place place(const Plan &p, uint32_t block, uint32_t first_channel, uint32_t end_channel)
 {
     Place q;
     q.n = p.div_chunks.div(block);
     q.chunk = block - q.n * p.chunks;
     q.r = p.div_nv.div(threadIdx.x);
     q.v = threadIdx.x - q.r * p.nv;
-    q.row_beg = q.chunk * p.rows_per;
-    q.row_end = a.spatial - q.row_beg < p.rows_per ? a.spatial : q.row_beg + p.rows_per;
-    // channels that exist from this vector on; threads behind the last position's have none
-    q.valid = q.r < p.rp && 8u * q.v < a.channels ? (int)(a.channels - 8u * q.v) : 0;
+    q.c = first_channel + 8u * q.v;
+    // threads behind the last position's have no channels
+    q.valid = q.r < p.rp && q.c < end_channel ? (int)(end_channel - q.c) : 0;
     return q;
 }
 
-// Sums over the workgroup's threads of eight values per thread: over the rp positions for every channel, into s[c].
+// Sums over the workgroup's threads of eight values per thread and channel: over the rp positions for every channel, into
+// s[channel of the segment].  Two sums at once, the second behind the first's threads * 8 values.
 template <class V>
-__device__ __forceinline__ void join_channels(V *s, const V (&v)[8], const Plan &p)
+__device__ __forceinline__ void join_channels(V *s, const V (&v)[8], const V (&w)[8], const Plan &p)
 {
+    V *s2 = s + blockDim.x * 8u;
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 8; ++k) s[threadIdx.x * 8u + k] = v[k];
+    for (int k = 0; k < 8; ++k) { s[threadIdx.x * 8u + k] = v[k]; s2[threadIdx.x * 8u + k] = w[k]; }
     __syncthreads();
     const uint32_t width = p.nv * 8u;
-    for (uint32_t c = threadIdx.x; c < width; c += blockDim.x) {
+    for (uint32_t c = threadIdx.x; c < 2u * width; c += blockDim.x) {
+        V *q = c < width ? s + c : s2 + (c - width);
         double t = 0.0;
-        for (uint32_t r = 0; r < p.rp; ++r) t += (double)s[r * width + c];
-        s[c] = (V)t;
+        for (uint32_t r = 0; r < p.rp; ++r) t += (double)q[r * width];
+        *q = (V)t;
     }
     __syncthreads();
 }
 
-// Sum over a group's channels of f(c), by one wave.
+// Sum over a group's channels of f(channel of the segment), by one wave; g counts from the segment's first group.
 template <class FN>
 __device__ __forceinline__ double group_total(uint32_t g, uint32_t per, FN f)
 {
@@ -105,222 +163,463 @@ __device__ __forceinline__ double group_total(uint32_t g, uint32_t per, FN f)
 
 // Sums and sums of squares in fp64, which the vector units add at the rate of fp32: no cancellation however far
 // the mean lies from zero, and no second pass over the data for the variance.
-template <uint32_t T>
+__device__ __forceinline__ void add_moments(f32x8 v, double (&s1)[8], double (&s2)[8])
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const double d = (double)v[k];
+        s1[k] += d;
+        s2[k] = __builtin_fma(d, d, s2[k]);
+    }
+}
+
+// Totals of the workgroup for each of `groups` groups of its segment: give(g, sum, sum of squares) by the first lane
+// of a wave.  Where a vector's channels are all of one group, they are added up before LDS.
+template <class FN>
+__device__ __forceinline__ void join_moments(double *s, double (&s1)[8], double (&s2)[8], uint32_t groups, const Plan &p, FN give)
+{
+    const uint32_t wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63u;
+    if ((p.per & 7u) == 0) {
+        double t1 = 0.0, t2 = 0.0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { t1 += s1[k]; t2 += s2[k]; }
+        s[2u * threadIdx.x] = t1;
+        s[2u * threadIdx.x + 1u] = t2;
+        __syncthreads();
+        const uint32_t pv = p.per / 8u, items = pv * p.rp;
+        for (uint32_t g = wave; g < groups; g += waves) {
+            t1 = t2 = 0.0;
+            for (uint32_t i = lane; i < items; i += 64u) {
+                const uint32_t r = i / pv, t = r * p.nv + g * pv + (i - r * pv);
+                t1 += s[2u * t];
+                t2 += s[2u * t + 1u];
+            }
+            t1 = wave_sum(t1);
+            t2 = wave_sum(t2);
+            if (lane == 0) give(g, t1, t2);
+        }
+    } else {
+        join_channels(s, s1, s2, p);
+        const double *u = s + blockDim.x * 8u;
+        for (uint32_t g = wave; g < groups; g += waves) {
+            const double t1 = group_total(g, p.per, [&](uint32_t c) { return s[c]; });
+            const double t2 = group_total(g, p.per, [&](uint32_t c) { return u[c]; });
+            if (lane == 0) give(g, t1, t2);
+        }
+    }
+}
+
+struct Moments { double mean, rstd; };
+__device__ __forceinline__ Moments moments_of(const NormArgs &a, const Plan &p, double s1, double s2)
+{
+    const double mean = s1 * p.share;
+    double var = s2 * p.share - mean * mean;
+    if (var < 0.0) var = 0.0;
+    var += a.eps;
+    // an approximation of 26 bits and two steps of Newton's method: a division and a square root take four times as long
+    double r = __builtin_amdgcn_rsq(var);
+    r = r * __builtin_fma(-0.5 * var * r, r, 1.5);
+    r = r * __builtin_fma(-0.5 * var * r, r, 1.5);
+    return {mean, r};
+}
+
+// u = (x - mean) * mul + add of a thread's channels (a group of equal values gives exactly `add`).  m: mean and
+// 1 / deviation of the groups, the first that of channel `first`.
+struct Line { float mean[8], mul[8], add[8]; };
+__device__ __forceinline__ Line parameters_of(const NormArgs &a, const Place &q)
+{
+    Line l;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        l.mean[k] = l.mul[k] = l.add[k] = 0.0f;
+        if (k < q.valid) {
+            l.mul[k] = a.gamma ? a.gamma[q.c + k] : 1.0f;
+            l.add[k] = a.beta ? a.beta[q.c + k] : 0.0f;
+        }
+    }
+    return l;
+}
+__device__ __forceinline__ void apply_moments(Line *l, const Plan &p, const Place &q, const double *m, uint32_t first)
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        if (k < q.valid) {
+            const uint32_t g = p.div_per.div(q.c + k - first);
+            l->mean[k] = (float)m[2 * g];
+            l->mul[k] = (float)(m[2 * g + 1] * (double)l->mul[k]);
+        }
+    }
+}
+
+// y and codes of one vector; all lanes of a quantisation group come here together.  `in`: its position exists.
+template <uint32_t T, uint32_t F, bool EVEN>
+__device__ __forceinline__ void put_outputs(const NormArgs &a, const Place &q, const Line &l, f32x8 x, uint64_t row, bool in)
+{
+    typedef typename ElemOf<T>::type E;
+    const int n = in ? q.valid : 0;
+    f32x8 y;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] = activate(__builtin_fmaf(x[k] - l.mean[k], l.mul[k], l.add[k]), a.act);
+    if (n > 0) store8<T>(static_cast<E *>(a.y) + row * a.channels + q.c, y, EVEN ? 8 : n);
+    if constexpr (F != kPlain) {
+        const uint32_t e = group_exponent<F>(lanes_max(amax8(x, 0u), a.gshift - 3));
+        if (in && q.c < a.pitch) {
+            *reinterpret_cast<u32x2 *>(a.codes + row * a.pitch + q.c) = encode8<F>(x, inverse_scale_of(e));
+            if (n > 0 && (q.c & ((1u << a.gshift) - 1u)) == 0) a.exps[row * a.ngroups + (q.c >> a.gshift)] = (uint8_t)e;
+        }
+    }
+}
+
+// load8 where either all eight values exist or none (EVEN: channels are a multiple of eight).
+template <uint32_t T, bool EVEN>
+__device__ __forceinline__ f32x8 load_vector(const typename ElemOf<T>::type *p, int n)
+{
+    if constexpr (EVEN) {
+        f32x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (n > 0) v = load8<T>(p, 8);
+        return v;
+    } else {
+        return load8<T>(p, n);
+    }
+}
+
+__device__ __forceinline__ void put_tail(const NormArgs &a)
+{
+    if (blockIdx.x == 0 && threadIdx.x < a.tail_to - a.tail_from) a.codes[a.tail_from + threadIdx.x] = 0;
+}
+
+template <uint32_t T, uint32_t F, bool EVEN>
+__global__ __launch_bounds__(kMaxThreads) void k_norm_slab(NormArgs a, Plan p)
+{
+    extern __shared__ double s_sum[];
+    typedef typename ElemOf<T>::type E;
+    Place q = place(p, blockIdx.x, 0, 0);
+    const uint32_t first = q.chunk * p.nv * 8u, end = a.channels - first < p.nv * 8u ? a.channels : first + p.nv * 8u;
+    q = place(p, blockIdx.x, first, end);
+    const uint64_t row0 = (uint64_t)q.n * a.spatial;
+    f32x8 x[kSlabRows];
+    double s1[8], s2[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s1[k] = s2[k] = 0.0;
+#pragma unroll
+    for (uint32_t i = 0; i < kSlabRows; ++i) {
+        const uint32_t r = q.r + i * p.rp;
+        const int n = r < a.spatial ? q.valid : 0;
+        x[i] = load_vector<T, EVEN>(static_cast<const E *>(a.x) + (n > 0 ? (row0 + r) * a.channels + q.c : 0), n);
+    }
+    Line l = parameters_of(a, q);
+#pragma unroll
+    for (uint32_t i = 0; i < kSlabRows; ++i) add_moments(x[i], s1, s2);
+    const uint32_t groups = (end - first) / p.per;
+    double *m = s_sum + (p.per & 7u ? 16u : 2u) * blockDim.x;
+    join_moments(s_sum, s1, s2, groups, p, [&](uint32_t g, double t1, double t2) {
+        const Moments v = moments_of(a, p, t1, t2);
+        m[2 * g] = v.mean;
+        m[2 * g + 1] = v.rstd;
+        if (a.stats) {
+            double *st = a.stats + ((uint64_t)q.n * a.groups + p.div_per.div(first) + g) * 2;
+            st[0] = v.mean;
+            st[1] = v.rstd;
+        }
+    });
+    __syncthreads();
+    apply_moments(&l, p, q, m, first);
+    if (F != kPlain) put_tail(a);
+#pragma unroll
+    for (uint32_t i = 0; i < kSlabRows; ++i) {
+        if (i * p.rp >= a.spatial) break;                                 // (uniform)
+        const uint32_t r = q.r + i * p.rp;
+        put_outputs<T, F, EVEN>(a, q, l, x[i], row0 + r, r < a.spatial && q.r < p.rp);
+    }
+}
+
+template <uint32_t T, bool EVEN>
 __global__ __launch_bounds__(kMaxThreads) void k_norm_sums(NormArgs a, Plan p)
 {
     extern __shared__ double s_sum[];
     typedef typename ElemOf<T>::type E;
-    const Place q = place(a, p, blockIdx.x);
+    const Place q = place(p, blockIdx.x, 0, a.channels);
+    const uint32_t beg = q.chunk * p.rows_per, end = a.spatial - beg < p.rows_per ? a.spatial : beg + p.rows_per;
     double s1[8], s2[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) s1[k] = s2[k] = 0.0;
     if (q.valid > 0) {
-        const E *x = static_cast<const E *>(a.x) + (uint64_t)q.n * a.spatial * a.channels + 8u * q.v;
-        for (uint32_t r = q.row_beg + q.r; r < q.row_end; r += p.rp) {
-            const f32x8 v = load8<T>(x + (uint64_t)r * a.channels, q.valid);
+        const E *x = static_cast<const E *>(a.x) + ((uint64_t)q.n * a.spatial + beg + q.r) * a.channels + q.c;
+        const uint64_t step = (uint64_t)p.rp * a.channels;
+        const int n = EVEN ? 8 : q.valid;
+        uint32_t left = end - beg > q.r ? (end - beg - q.r + p.rp - 1) / p.rp : 0;      // positions of this thread
+        for (; left >= 4; left -= 4, x += 4 * step) {                     // four loads in flight
+            f32x8 v[4];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const double d = (double)v[k];
-                s1[k] += d;
-                s2[k] = __builtin_fma(d, d, s2[k]);
-            }
+            for (uint32_t i = 0; i < 4; ++i) v[i] = load8<T>(x + i * step, n);
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) add_moments(v[i], s1, s2);
         }
+        for (; left; --left, x += step) add_moments(load8<T>(x, n), s1, s2);
     }
-    const uint32_t per = a.channels / a.groups, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     double *part = static_cast<double *>(a.work);
-    for (int which = 0; which < 2; ++which) {
-        join_channels(s_sum, which ? s2 : s1, p);
-        for (uint32_t g = wave; g < a.groups; g += waves) {
-            const double t = group_total(g, per, [&](uint32_t c) { return s_sum[c]; });
-            if ((threadIdx.x & 63u) == 0) part[(((uint64_t)q.n * a.groups + g) * p.chunks + q.chunk) * 2 + which] = t;
-        }
-    }
+    join_moments(s_sum, s1, s2, a.groups, p, [&](uint32_t g, double t1, double t2) {
+        double *o = part + (((uint64_t)q.n * a.groups + g) * p.chunks + q.chunk) * 2;
+        o[0] = t1;
+        o[1] = t2;
+    });
 }
 
-// Two totals over the workgroups of a sample, for every group, into s[2 * g], s[2 * g + 1].
+// Two totals over the workgroups of a sample, for every group, into s[2 * g], s[2 * g + 1]: as many lanes to a group as
+// the workgroup has for all of them at once.
 __device__ __forceinline__ void join_chunks(double *s, const double *part, uint32_t n, const NormArgs &a, const Plan &p)
 {
-    const uint32_t wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63u;
-    for (uint32_t g = wave; g < a.groups; g += waves) {
-        const double *at = part + ((uint64_t)n * a.groups + g) * p.chunks * 2;
+    uint32_t lanes = 64;
+    while (lanes > 1 && a.groups * lanes > blockDim.x) lanes >>= 1;
+    const uint32_t side = blockDim.x / lanes, lane = threadIdx.x & (lanes - 1u);
+    for (uint32_t g0 = 0; g0 < a.groups; g0 += side) {
+        const uint32_t g = g0 + threadIdx.x / lanes;
         double t1 = 0.0, t2 = 0.0;
-        for (uint32_t c = lane; c < p.chunks; c += 64u) { t1 += at[2 * c]; t2 += at[2 * c + 1]; }
-        t1 = wave_sum(t1);
-        t2 = wave_sum(t2);
-        if (lane == 0) { s[2 * g] = t1; s[2 * g + 1] = t2; }
+        if (g < a.groups) {
+            const double *at = part + ((uint64_t)n * a.groups + g) * p.chunks * 2;
+#pragma unroll 4
+            for (uint32_t c = lane; c < p.chunks; c += lanes) { t1 += at[2 * c]; t2 += at[2 * c + 1]; }
+        }
+        for (uint32_t k = lanes >> 1; k > 0; k >>= 1) { t1 += __shfl_xor(t1, k); t2 += __shfl_xor(t2, k); }
+        if (g < a.groups && lane == 0) { s[2 * g] = t1; s[2 * g + 1] = t2; }
     }
     __syncthreads();
 }
 
-__device__ __forceinline__ float activate(float u, uint32_t act)
-{
-    return act == kActSilu ? u * sigmoid(u) : act == kActRelu ? (u > 0.0f ? u : u != u ? u : 0.0f) : u;
-}
-
-template <uint32_t T, uint32_t F>
+template <uint32_t T, uint32_t F, bool EVEN>
 __global__ __launch_bounds__(kMaxThreads) void k_norm_apply(NormArgs a, Plan p)
 {
     extern __shared__ double s_sum[];
     typedef typename ElemOf<T>::type E;
-    const Place q = place(a, p, blockIdx.x);
+    const Place q = place(p, blockIdx.x, 0, a.channels);
+    const uint32_t beg = q.chunk * p.rows_per, end = a.spatial - beg < p.rows_per ? a.spatial : beg + p.rows_per;
+    const uint64_t row0 = (uint64_t)q.n * a.spatial;
+    const E *src = static_cast<const E *>(a.x) + (q.valid > 0 ? q.c : 0);
+    auto fetch = [&](uint32_t base) {
+        const uint32_t r = base + q.r;
+        const int n = r < end ? q.valid : 0;
+        return load_vector<T, EVEN>(src + (n > 0 ? (row0 + r) * a.channels : 0), n);
+    };
+    Line l = parameters_of(a, q);
     join_chunks(s_sum, static_cast<const double *>(a.work), q.n, a, p);
-    const double count = (double)a.spatial * (double)(a.channels / a.groups);
     for (uint32_t g = threadIdx.x; g < a.groups; g += blockDim.x) {
-        const double mean = s_sum[2 * g] / count;
-        double var = s_sum[2 * g + 1] / count - mean * mean;
-        if (var < 0.0) var = 0.0;
-        const double rstd = 1.0 / sqrt(var + a.eps);
-        s_sum[2 * g] = mean;
-        s_sum[2 * g + 1] = rstd;
+        const Moments v = moments_of(a, p, s_sum[2 * g], s_sum[2 * g + 1]);
+        s_sum[2 * g] = v.mean;
+        s_sum[2 * g + 1] = v.rstd;
         if (q.chunk == 0 && a.stats) {
-            a.stats[((uint64_t)q.n * a.groups + g) * 2] = mean;
-            a.stats[((uint64_t)q.n * a.groups + g) * 2 + 1] = rstd;
+            a.stats[((uint64_t)q.n * a.groups + g) * 2] = v.mean;
+            a.stats[((uint64_t)q.n * a.groups + g) * 2 + 1] = v.rstd;
         }
     }
     __syncthreads();
-    float mean[8], mul[8], add[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const uint32_t c = 8u * q.v + k;
-        mean[k] = mul[k] = add[k] = 0.0f;
-        if (k < q.valid) {
-            const uint32_t g = p.div_per.div(c);
-            mean[k] = (float)s_sum[2 * g];
-            mul[k] = (float)s_sum[2 * g + 1] * (a.gamma ? a.gamma[c] : 1.0f);
-            add[k] = a.beta ? a.beta[c] : 0.0f;
-        }
-    }
-    if (F != kPlain && blockIdx.x == 0 && threadIdx.x < a.tail_to - a.tail_from) a.codes[a.tail_from + threadIdx.x] = 0;
-    const uint64_t row0 = (uint64_t)q.n * a.spatial;
-    // every thread of the workgroup goes round as often: the lanes of a quantisation group meet in lanes_max
-    for (uint32_t base = q.row_beg; base < q.row_end; base += p.rp) {
+    apply_moments(&l, p, q, s_sum, 0);
+    if (F != kPlain) put_tail(a);
+    // every thread of the workgroup goes round as often: the lanes of a quantisation group meet in put_outputs
+    f32x8 next = fetch(beg);
+    for (uint32_t base = beg; base < end; base += p.rp) {
+        const f32x8 x = next;
+        next = fetch(base + p.rp);                                        // behind the end: nothing
         const uint32_t r = base + q.r;
-        const bool in = r < q.row_end && q.r < p.rp;
-        const int n = in ? q.valid : 0;
-        const uint64_t row = row0 + r;
-        const f32x8 x = load8<T>(static_cast<const E *>(a.x) + (n > 0 ? row * a.channels + 8u * q.v : 0), n);
-        f32x8 y;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] = activate(__builtin_fmaf(x[k] - mean[k], mul[k], add[k]), a.act);
-        store8<T>(static_cast<E *>(a.y) + (n > 0 ? row * a.channels + 8u * q.v : 0), y, n);
-        if constexpr (F != kPlain) {
-            const uint32_t e = group_exponent<F>(lanes_max(amax8(x, 0u), a.gshift - 3));
-            if (in && 8u * q.v < a.pitch) {
-                *reinterpret_cast<u32x2 *>(a.codes + row * a.pitch + 8u * q.v) = encode8<F>(x, inverse_scale_of(e));
-                if (n > 0 && ((8u * q.v) & ((1u << a.gshift) - 1u)) == 0)
-                    a.exps[row * a.ngroups + ((8u * q.v) >> a.gshift)] = (uint8_t)e;
-            }
-        }
+        put_outputs<T, F, EVEN>(a, q, l, x, row0 + r, r < end && q.r < p.rp);
     }
 }
 
 // ---- backward -----------------------------------------------------------------------------------------
 
-template <uint32_t T, uint32_t S>
-__device__ __forceinline__ f32x8 source8(const NormArgs &a, uint64_t row, uint32_t v, int n)
-{
-    typedef typename ElemOf<T>::type E;
-    if constexpr (S == kPlain) {
-        return load8<T>(static_cast<const E *>(a.x) + (n > 0 ? row * a.channels + 8u * v : 0), n);
-    } else {
-        if (n <= 0) return f32x8{0, 0, 0, 0, 0, 0, 0, 0};
-        const u32x2 w = *reinterpret_cast<const u32x2 *>(a.codes + row * a.pitch + 8u * v);
-        return decode8<S>(w, scale_of(a.exps[row * a.ngroups + ((8u * v) >> a.gshift)]));
+// Eight values of the input as `v` * `s`: codes and their scale, or the values themselves and 1.
+struct Source { f32x8 v; float s; };
+template <uint32_t T, uint32_t S> struct Held {                           // as they lie in memory
+    u32x4 w[T == kTypeF32 ? 2 : 1];
+    // EVEN: eight values or none
+    template <bool EVEN>
+    __device__ __forceinline__ void load(const void *x, const NormArgs &a, uint64_t row, uint32_t c, int n)
+    {
+        typedef typename ElemOf<T>::type E;
+        const E *p = static_cast<const E *>(x) + (n > 0 ? row * a.channels + c : 0);
+        if constexpr (EVEN) {
+#pragma unroll
+            for (int k = 0; k < (int)(sizeof(w) / 16); ++k) w[k] = u32x4{0, 0, 0, 0};
+            if (n > 0) __builtin_memcpy(w, p, sizeof(w));
+            return;
+        }
+        if (n >= 8) { __builtin_memcpy(w, p, sizeof(w)); return; }
+        E e[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e[k] = k < n ? p[k] : (E)0.0f;
+        __builtin_memcpy(w, e, sizeof(w));
     }
-}
+    __device__ __forceinline__ Source values() const
+    {
+        typename ElemOf<T>::type e[8];
+        __builtin_memcpy(e, w, sizeof(w));
+        Source r;
+        r.s = 1.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) r.v[k] = (float)e[k];
+        return r;
+    }
+};
+template <uint32_t S> struct HeldCodes {
+    u32x2 w;
+    uint32_t e;
+    template <bool>
+    __device__ __forceinline__ void load(const void *, const NormArgs &a, uint64_t row, uint32_t c, int n)
+    {
+        w = u32x2{0, 0};
+        e = 127;
+        if (n > 0) {
+            w = *reinterpret_cast<const u32x2 *>(a.codes + row * a.pitch + c);
+            e = a.exps[row * a.ngroups + (c >> a.gshift)];
+        }
+    }
+    __device__ __forceinline__ Source values() const
+    {
+        Source r;
+        r.s = scale_of(e);
+        if constexpr (S == kByteInt8) {
+            uint32_t found = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t u = w[h] ^ 0x80808080u;                    // code + 128
+                found |= (u - 0x01010101u) & ~u;                          // a byte of zero leaves its highest bit
+#pragma unroll
+                for (int k = 0; k < 4; ++k) r.v[4 * h + k] = (float)(int8_t)(w[h] >> (8 * k));
+            }
+            if (found & 0x80808080u) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (r.v[k] == -128.0f) r.v[k] = __uint_as_float(0x7fc00000u);
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x2 p = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[h], false), q = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[h], true);
+                r.v[4 * h] = p[0]; r.v[4 * h + 1] = p[1]; r.v[4 * h + 2] = q[0]; r.v[4 * h + 3] = q[1];
+            }
+        }
+        return r;
+    }
+};
+template <uint32_t T, uint32_t S> using HeldAs = typename std::conditional<S == kPlain, Held<T, S>, HeldCodes<S>>::type;
 
-// A thread's eight channels.
-struct Channels { float mean[8], rstd[8], gamma[8], beta[8]; };
-__device__ __forceinline__ Channels channels_of(const NormArgs &a, const Plan &p, const Place &q)
+// h = x * hr + hm, u = h * gamma + beta of a thread's channels.  ONE: all of a vector's channels are in one group.
+template <bool ONE> struct Channels { float hr[ONE ? 1 : 8], hm[ONE ? 1 : 8], gamma[8], beta[8]; };
+template <bool ONE>
+__device__ __forceinline__ Channels<ONE> channels_of(const NormArgs &a, const Plan &p, const Place &q)
 {
-    Channels c;
+    Channels<ONE> c;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const uint32_t ch = 8u * q.v + k;
-        c.mean[k] = c.rstd[k] = c.gamma[k] = c.beta[k] = 0.0f;
+        c.gamma[k] = c.beta[k] = 0.0f;
         if (k < q.valid) {
-            const double *st = a.stats + ((uint64_t)q.n * a.groups + p.div_per.div(ch)) * 2;
-            c.mean[k] = (float)st[0];
-            c.rstd[k] = (float)st[1];
-            c.gamma[k] = a.gamma ? a.gamma[ch] : 1.0f;
-            c.beta[k] = a.beta ? a.beta[ch] : 0.0f;
+            c.gamma[k] = a.gamma ? a.gamma[q.c + k] : 1.0f;
+            c.beta[k] = a.beta ? a.beta[q.c + k] : 0.0f;
+        }
+        if (k < (ONE ? 1 : 8)) {
+            c.hr[k] = c.hm[k] = 0.0f;
+            if (k < q.valid) {
+                const double *st = a.stats + ((uint64_t)q.n * a.groups + p.div_per.div(q.c + k)) * 2;
+                c.hr[k] = (float)st[1];
+                c.hm[k] = (float)(-st[0] * st[1]);
+            }
         }
     }
     return c;
 }
 
 // du = dy * act'(u) and h of eight channels.
-__device__ __forceinline__ void gradient8(const NormArgs &a, const Plan &p, const Place &q, const Channels &c, f32x8 x, f32x8 dy,
-                                          f32x8 *du, f32x8 *h)
+template <uint32_t ACT, bool ONE>
+__device__ __forceinline__ void gradient8(const NormArgs &a, const Plan &p, const Place &q, const Channels<ONE> &c, const Source &x,
+                                          f32x8 dy, f32x8 *du, f32x8 *h)
+{
+    const float one = x.s * c.hr[0];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float hr = ONE ? one : x.s * c.hr[ONE ? 0 : k], hm = c.hm[ONE ? 0 : k];
+        const float hk = __builtin_fmaf(x.v[k], hr, hm);
+        (*h)[k] = hk;
+        if constexpr (ACT == kActNone) {
+            (*du)[k] = dy[k];
+        } else {
+            const float u = __builtin_fmaf(hk, c.gamma[k], c.beta[k]);
+            if constexpr (ACT == kActSilu) {
+                const float g = sigmoid(u);
+                (*du)[k] = dy[k] * (g * __builtin_fmaf(u, 1.0f - g, 1.0f));
+            } else {
+                bool positive = u > 0.0f;
+                // where fp32 cannot tell the side of the border (its error is below eight roundings of these terms), fp64 does
+                const float terms = __builtin_fmaf(fabsf(c.gamma[k]), __builtin_fmaf(fabsf(x.v[k]), fabsf(hr), fabsf(hm)), fabsf(c.beta[k]));
+                if (fabsf(u) < 0x1p-20f * terms && k < q.valid) {
+                    float gamma = c.gamma[k], beta = c.beta[k];
+                    uint32_t ch = q.c + k;
+                    asm volatile("" : "+v"(gamma), "+v"(beta), "+v"(ch));   // rare: nothing of this is worth registers outside
+                    const double *st = a.stats + ((uint64_t)q.n * a.groups + p.div_per.div(ch)) * 2;
+                    const double v = (double)x.v[k] * (double)x.s;
+                    positive = (v - st[0]) * st[1] * (double)gamma + (double)beta > 0.0;
+                }
+                (*du)[k] = positive ? dy[k] : u != u ? u : 0.0f;
+            }
+        }
+    }
+}
+
+// gamma of the segment's channels in LDS, for the waves that add up groups (a barrier follows).
+template <bool ONE>
+__device__ __forceinline__ const float *put_gamma(float *s, const Plan &p, const Place &q, const Channels<ONE> &c)
+{
+    if (threadIdx.x < p.nv) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[8u * threadIdx.x + k] = c.gamma[k];
+    }
+    return s;
+}
+
+__device__ __forceinline__ void add_sums(f32x8 du, f32x8 h, float (&sp)[8], float (&sq)[8])
 {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const float hk = (x[k] - c.mean[k]) * c.rstd[k], u = __builtin_fmaf(hk, c.gamma[k], c.beta[k]);
-        (*h)[k] = hk;
-        if (a.act == kActSilu) {
-            const float g = sigmoid(u);
-            (*du)[k] = dy[k] * (g * __builtin_fmaf(u, 1.0f - g, 1.0f));
-        } else if (a.act == kActRelu) {
-            bool positive = u > 0.0f;
-            // where fp32 cannot tell the side of the border (its error is below eight roundings of these terms), fp64 does
-            const float terms = __builtin_fmaf(fabsf(c.gamma[k] * c.rstd[k]), fabsf(x[k]) + fabsf(c.mean[k]), fabsf(c.beta[k]));
-            if (fabsf(u) < 0x1p-20f * terms && k < q.valid) {
-                const double *st = a.stats + ((uint64_t)q.n * a.groups + p.div_per.div(8u * q.v + k)) * 2;
-                positive = ((double)x[k] - st[0]) * st[1] * (double)c.gamma[k] + (double)c.beta[k] > 0.0;
-            }
-            (*du)[k] = positive ? dy[k] : u != u ? u : 0.0f;
-        } else {
-            (*du)[k] = dy[k];
+        sp[k] += du[k];
+        sq[k] = __builtin_fmaf(du[k], h[k], sq[k]);
+    }
+}
+
+// dx = hr * (du * gamma - (A + h * B)); ga, gb: A and B of the channels' groups, divided by the count.
+template <bool ONE>
+__device__ __forceinline__ f32x8 input_gradient(const Channels<ONE> &c, f32x8 du, f32x8 h, const float (&ga)[ONE ? 1 : 8],
+                                                const float (&gb)[ONE ? 1 : 8])
+{
+    f32x8 dx;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float t = __builtin_fmaf(du[k], c.gamma[k], -ga[ONE ? 0 : k]);
+        dx[k] = c.hr[ONE ? 0 : k] * __builtin_fmaf(-h[k], gb[ONE ? 0 : k], t);
+    }
+    return dx;
+}
+
+// A and B over the count, for a thread's channels, from s[2 * g], s[2 * g + 1]; channel `first` is the first group's.
+template <bool ONE>
+__device__ __forceinline__ void pick_totals(const double *s, const NormArgs &a, const Plan &p, const Place &q, uint32_t first,
+                                            float (&ga)[ONE ? 1 : 8], float (&gb)[ONE ? 1 : 8])
+{
+#pragma unroll
+    for (int k = 0; k < (ONE ? 1 : 8); ++k) {
+        ga[k] = gb[k] = 0.0f;
+        if (k < q.valid) {
+            const uint32_t g = p.div_per.div(q.c + k - first);
+            ga[k] = (float)(s[2 * g] * p.share);
+            gb[k] = (float)(s[2 * g + 1] * p.share);
         }
     }
 }
 
-template <uint32_t T, uint32_t S>
-__global__ __launch_bounds__(kMaxThreads) void k_norm_grad_sums(NormArgs a, Plan p)
+// dbeta and dgamma of sixteen channels: the sums of `records` workgroups or samples, in a fixed order.
+__device__ __forceinline__ void join_parameters(double *s, const NormArgs &a, const float *chan, uint64_t records, uint32_t block)
 {
-    extern __shared__ double s_sum[];
-    typedef typename ElemOf<T>::type E;
-    float *s = reinterpret_cast<float *>(s_sum);
-    const Place q = place(a, p, blockIdx.x);
-    const Channels ch = channels_of(a, p, q);
-    float sp[8], sq[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) sp[k] = sq[k] = 0.0f;
-    const uint64_t row0 = (uint64_t)q.n * a.spatial;
-    if (q.valid > 0) {
-        for (uint32_t r = q.row_beg + q.r; r < q.row_end; r += p.rp) {
-            const uint64_t row = row0 + r;
-            const f32x8 dy = load8<T>(static_cast<const E *>(a.dy) + row * a.channels + 8u * q.v, q.valid);
-            f32x8 du, h;
-            gradient8(a, p, q, ch, source8<T, S>(a, row, q.v, q.valid), dy, &du, &h);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                sp[k] += du[k];
-                sq[k] = __builtin_fmaf(du[k], h[k], sq[k]);
-            }
-        }
-    }
-    const uint32_t per = a.channels / a.groups, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    double *part = static_cast<double *>(a.work);
-    float *chan = reinterpret_cast<float *>(part + 2ull * a.batch * a.groups * p.chunks) + 2ull * blockIdx.x * a.channels;
-    for (int which = 0; which < 2; ++which) {
-        join_channels(s, which ? sq : sp, p);
-        for (uint32_t c = threadIdx.x; c < a.channels; c += blockDim.x) chan[(uint64_t)which * a.channels + c] = s[c];
-        for (uint32_t g = wave; g < a.groups; g += waves) {
-            const double t = group_total(g, per, [&](uint32_t c) { return (double)s[c] * (double)(a.gamma ? a.gamma[c] : 1.0f); });
-            if ((threadIdx.x & 63u) == 0) part[(((uint64_t)q.n * a.groups + g) * p.chunks + q.chunk) * 2 + which] = t;
-        }
-    }
-}
-
-// dbeta and dgamma of sixteen channels: the sums of the first pass's workgroups, in a fixed order.
-__device__ __forceinline__ void join_parameters(double *s, const NormArgs &a, const Plan &p, uint32_t block)
-{
-    const uint64_t records = a.spatial ? a.batch * p.chunks : 0;
-    const float *chan = reinterpret_cast<const float *>(static_cast<const double *>(a.work) + 2ull * a.batch * a.groups * p.chunks);
     const uint32_t c = block * 16u + (threadIdx.x & 15u), parts = blockDim.x >> 4;
     double t[2] = {0.0, 0.0};
     if (c < a.channels) {
+#pragma unroll 4
         for (uint64_t k = threadIdx.x >> 4; k < records; k += parts) {
             t[0] += (double)chan[2 * k * a.channels + c];
             t[1] += (double)chan[(2 * k + 1) * a.channels + c];
@@ -339,76 +638,239 @@ __device__ __forceinline__ void join_parameters(double *s, const NormArgs &a, co
     }
 }
 
-template <uint32_t T, uint32_t S>
+__global__ __launch_bounds__(kMaxThreads) void k_norm_parameters(NormArgs a, uint64_t records)
+{
+    extern __shared__ double s_sum[];
+    join_parameters(s_sum, a, static_cast<const float *>(a.work), records, blockIdx.x);
+}
+
+template <uint32_t T, uint32_t S, uint32_t ACT, bool ONE>
+__global__ __launch_bounds__(kMaxThreads) void k_norm_grad_slab(NormArgs a, Plan p)
+{
+    extern __shared__ double s_sum[];
+    typedef typename ElemOf<T>::type E;
+    Place q = place(p, blockIdx.x, 0, 0);
+    const uint32_t first = q.chunk * p.nv * 8u, end = a.channels - first < p.nv * 8u ? a.channels : first + p.nv * 8u;
+    q = place(p, blockIdx.x, first, end);
+    const uint64_t row0 = (uint64_t)q.n * a.spatial;
+    const Channels<ONE> ch = channels_of<ONE>(a, p, q);
+    Held<T, kPlain> dy[kSlabRows];
+    HeldAs<T, S> x[kSlabRows];
+#pragma unroll
+    for (uint32_t i = 0; i < kSlabRows; ++i) {
+        const uint32_t r = q.r + i * p.rp;
+        const int n = r < a.spatial ? q.valid : 0;
+        dy[i].template load<ONE>(a.dy, a, row0 + r, q.c, n);
+        x[i].template load<ONE>(a.x, a, row0 + r, q.c, n);
+    }
+    float sp[8], sq[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sp[k] = sq[k] = 0.0f;
+    f32x8 du, h;
+#pragma unroll
+    for (uint32_t i = 0; i < kSlabRows; ++i) {
+        if (i * p.rp >= a.spatial) break;                                 // (uniform)
+        gradient8<ACT, ONE>(a, p, q, ch, x[i].values(), dy[i].values().v, &du, &h);
+        add_sums(du, h, sp, sq);
+    }
+    float *s = reinterpret_cast<float *>(s_sum);
+    double *tot = s_sum + 8u * blockDim.x + 4u * p.nv;
+    const float *s2 = s + blockDim.x * 8u, *sg = put_gamma(s + blockDim.x * 16u, p, q, ch);
+    join_channels(s, sp, sq, p);
+    const uint32_t groups = (end - first) / p.per, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    for (uint32_t c = threadIdx.x; c < end - first; c += blockDim.x) {
+        if (a.batch == 1) {
+            if (a.dbeta) a.dbeta[first + c] = s[c];
+            if (a.dgamma) a.dgamma[first + c] = s2[c];
+        } else {
+            float *chan = static_cast<float *>(a.work) + 2ull * q.n * a.channels + first + c;
+            chan[0] = s[c];
+            chan[a.channels] = s2[c];
+        }
+    }
+    for (uint32_t g = wave; g < groups; g += waves) {
+        const double t1 = group_total(g, p.per, [&](uint32_t c) { return (double)s[c] * (double)sg[c]; });
+        const double t2 = group_total(g, p.per, [&](uint32_t c) { return (double)s2[c] * (double)sg[c]; });
+        if ((threadIdx.x & 63u) == 0) { tot[2 * g] = t1; tot[2 * g + 1] = t2; }
+    }
+    __syncthreads();
+    float ga[ONE ? 1 : 8], gb[ONE ? 1 : 8];
+    pick_totals<ONE>(tot, a, p, q, first, ga, gb);
+#pragma unroll
+    for (uint32_t i = 0; i < kSlabRows; ++i) {
+        const uint32_t r = q.r + i * p.rp;
+        if (r >= a.spatial || q.valid <= 0) break;
+        gradient8<ACT, ONE>(a, p, q, ch, x[i].values(), dy[i].values().v, &du, &h);
+        store8<T>(static_cast<E *>(a.y) + (row0 + r) * a.channels + q.c, input_gradient<ONE>(ch, du, h, ga, gb), q.valid);
+    }
+}
+
+// Two positions of a thread at a time, all their loads in flight: take(position, du, h).
+template <uint32_t T, uint32_t S, uint32_t ACT, bool ONE, class FN>
+__device__ __forceinline__ void each_gradient(const NormArgs &a, const Plan &p, const Place &q, const Channels<ONE> &ch, FN take)
+{
+    const uint32_t beg = q.chunk * p.rows_per, end = a.spatial - beg < p.rows_per ? a.spatial : beg + p.rows_per;
+    const uint64_t row0 = (uint64_t)q.n * a.spatial;
+    if (q.valid <= 0 || q.r >= end - beg) return;
+    uint32_t left = (end - beg - q.r + p.rp - 1) / p.rp;                  // positions of this thread
+    uint64_t row = row0 + beg + q.r;
+    const int n = ONE ? 8 : q.valid;
+    auto one = [&](const Held<T, kPlain> &dy, const HeldAs<T, S> &x, uint64_t at) {
+        f32x8 du, h;
+        gradient8<ACT, ONE>(a, p, q, ch, x.values(), dy.values().v, &du, &h);
+        take(at, du, h);
+    };
+    for (; left >= 2; left -= 2, row += 2 * p.rp) {
+        Held<T, kPlain> dy[2];
+        HeldAs<T, S> x[2];
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i) {
+            dy[i].template load<false>(a.dy, a, row + i * p.rp, q.c, n);
+            x[i].template load<false>(a.x, a, row + i * p.rp, q.c, n);
+        }
+        one(dy[0], x[0], row);
+        one(dy[1], x[1], row + p.rp);
+    }
+    if (left) {
+        Held<T, kPlain> dy;
+        HeldAs<T, S> x;
+        dy.template load<false>(a.dy, a, row, q.c, n);
+        x.template load<false>(a.x, a, row, q.c, n);
+        one(dy, x, row);
+    }
+}
+
+template <uint32_t T, uint32_t S, uint32_t ACT, bool ONE>
+__global__ __launch_bounds__(kMaxThreads) void k_norm_grad_sums(NormArgs a, Plan p)
+{
+    extern __shared__ double s_sum[];
+    const Place q = place(p, blockIdx.x, 0, a.channels);
+    const Channels<ONE> ch = channels_of<ONE>(a, p, q);
+    float sp[8], sq[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sp[k] = sq[k] = 0.0f;
+    each_gradient<T, S, ACT, ONE>(a, p, q, ch, [&](uint64_t, f32x8 du, f32x8 h) { add_sums(du, h, sp, sq); });
+    float *s = reinterpret_cast<float *>(s_sum);
+    const float *s2 = s + blockDim.x * 8u, *sg = put_gamma(s + blockDim.x * 16u, p, q, ch);
+    join_channels(s, sp, sq, p);
+    const uint32_t wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    double *part = static_cast<double *>(a.work);
+    float *chan = reinterpret_cast<float *>(part + 2ull * a.batch * a.groups * p.chunks) + 2ull * blockIdx.x * a.channels;
+    for (uint32_t c = threadIdx.x; c < a.channels; c += blockDim.x) {
+        chan[c] = s[c];
+        chan[a.channels + c] = s2[c];
+    }
+    for (uint32_t g = wave; g < a.groups; g += waves) {
+        const double t1 = group_total(g, p.per, [&](uint32_t c) { return (double)s[c] * (double)sg[c]; });
+        const double t2 = group_total(g, p.per, [&](uint32_t c) { return (double)s2[c] * (double)sg[c]; });
+        double *o = part + (((uint64_t)q.n * a.groups + g) * p.chunks + q.chunk) * 2;
+        if ((threadIdx.x & 63u) == 0) { o[0] = t1; o[1] = t2; }
+    }
+}
+
+template <uint32_t T, uint32_t S, uint32_t ACT, bool ONE>
 __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_apply(NormArgs a, Plan p, uint32_t param_blocks)
 {
     extern __shared__ double s_sum[];
     typedef typename ElemOf<T>::type E;
-    if (blockIdx.x < param_blocks) { join_parameters(s_sum, a, p, blockIdx.x); return; }
-    const Place q = place(a, p, blockIdx.x - param_blocks);
-    join_chunks(s_sum, static_cast<const double *>(a.work), q.n, a, p);
-    const Channels ch = channels_of(a, p, q);
-    const double count = (double)a.spatial * (double)(a.channels / a.groups);
-    float ga[8], gb[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        ga[k] = gb[k] = 0.0f;
-        if (k < q.valid) {
-            const uint32_t g = p.div_per.div(8u * q.v + k);
-            ga[k] = (float)(s_sum[2 * g] / count);
-            gb[k] = (float)(s_sum[2 * g + 1] / count);
-        }
+    const double *part = static_cast<const double *>(a.work);
+    if (blockIdx.x < param_blocks) {
+        join_parameters(s_sum, a, reinterpret_cast<const float *>(part + 2ull * a.batch * a.groups * p.chunks),
+                        a.spatial ? a.batch * p.chunks : 0, blockIdx.x);
+        return;
     }
-    if (q.valid <= 0) return;
-    const uint64_t row0 = (uint64_t)q.n * a.spatial;
-    for (uint32_t r = q.row_beg + q.r; r < q.row_end; r += p.rp) {
-        const uint64_t row = row0 + r;
-        const f32x8 dy = load8<T>(static_cast<const E *>(a.dy) + row * a.channels + 8u * q.v, q.valid);
-        f32x8 du, h, dx;
-        gradient8(a, p, q, ch, source8<T, S>(a, row, q.v, q.valid), dy, &du, &h);
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            dx[k] = ch.rstd[k] * (__builtin_fmaf(du[k], ch.gamma[k], -ga[k]) - h[k] * gb[k]);
-        store8<T>(static_cast<E *>(a.y) + row * a.channels + 8u * q.v, dx, q.valid);
-    }
+    const Place q = place(p, blockIdx.x - param_blocks, 0, a.channels);
+    join_chunks(s_sum, part, q.n, a, p);
+    const Channels<ONE> ch = channels_of<ONE>(a, p, q);
+    float ga[ONE ? 1 : 8], gb[ONE ? 1 : 8];
+    pick_totals<ONE>(s_sum, a, p, q, 0, ga, gb);
+    each_gradient<T, S, ACT, ONE>(a, p, q, ch, [&](uint64_t row, f32x8 du, f32x8 h) {
+        store8<T>(static_cast<E *>(a.y) + row * a.channels + q.c, input_gradient<ONE>(ch, du, h, ga, gb), q.valid);
+    });
 }
 
-size_t lds_bytes(const NormArgs &a, const Plan &p, uint32_t per_thread)
+// ---- launches -----------------------------------------------------------------------------------------
+
+// LDS of a workgroup: `per_thread` bytes for each of its threads, and two doubles per group (behind them, or instead).
+size_t lds_bytes(const Plan &p, size_t per_thread, size_t groups, bool both)
 {
-    const size_t joined = (size_t)p.threads * per_thread, groups = 16ull * a.groups;
-    return joined > groups ? joined : groups;
+    const size_t joined = p.threads * per_thread, totals = 16 * groups;
+    return both ? joined + totals : joined > totals ? joined : totals;
 }
+size_t moment_bytes(const Plan &p) { return p.per & 7u ? 128 : 16; }
 
-template <uint32_t T>
+template <uint32_t T, uint32_t F, bool EVEN>
 void forward_as(const NormArgs &a, hipStream_t st)
 {
-    const uint32_t lanes = a.codes ? 1u << (a.gshift - 3) : 1u;
-    const Plan p = make_plan(a, lanes);
+    const uint32_t lanes = F != kPlain ? 1u << (a.gshift - 3) : 1u;
+    Plan p;
+    if (slab_plan(&p, a, lanes)) {
+        hipLaunchKernelGGL((k_norm_slab<T, F, EVEN>), dim3((uint32_t)(a.batch * p.chunks)), dim3(p.threads),
+                           lds_bytes(p, moment_bytes(p), p.nv * 8u / p.per, true), st, a, p);
+        return;
+    }
+    p = two_pass_plan(a, lanes);
     const dim3 grid((uint32_t)(a.batch * p.chunks)), block(p.threads);
-    hipLaunchKernelGGL((k_norm_sums<T>), grid, block, lds_bytes(a, p, 64), st, a, p);
-    const size_t lds = 16ull * a.groups;
-    if (!a.codes) hipLaunchKernelGGL((k_norm_apply<T, kPlain>), grid, block, lds, st, a, p);
-    else if (a.format == kByteInt8) hipLaunchKernelGGL((k_norm_apply<T, kByteInt8>), grid, block, lds, st, a, p);
-    else hipLaunchKernelGGL((k_norm_apply<T, kByteE4M3>), grid, block, lds, st, a, p);
+    hipLaunchKernelGGL((k_norm_sums<T, EVEN>), grid, block, lds_bytes(p, moment_bytes(p), 0, false), st, a, p);
+    hipLaunchKernelGGL((k_norm_apply<T, F, EVEN>), grid, block, lds_bytes(p, 0, a.groups, false), st, a, p);
+}
+
+template <uint32_t T, uint32_t S, uint32_t ACT, bool ONE>
+void backward_as(const NormArgs &a, hipStream_t st)
+{
+    const uint32_t params = a.dgamma || a.dbeta ? (a.channels + 15) / 16 : 0;
+    Plan p;
+    if (a.batch && slab_plan(&p, a, 1)) {
+        hipLaunchKernelGGL((k_norm_grad_slab<T, S, ACT, ONE>), dim3((uint32_t)(a.batch * p.chunks)), dim3(p.threads),
+                           lds_bytes(p, 64, p.nv * 8u / p.per, true) + 32 * p.nv, st, a, p);
+        if (params && a.batch > 1) hipLaunchKernelGGL(k_norm_parameters, dim3(params), dim3(1024), 8 * 1024, st, a, a.batch);
+        return;
+    }
+    p = two_pass_plan(a, 1);
+    const uint32_t work = a.spatial ? (uint32_t)(a.batch * p.chunks) : 0;
+    if (work)
+        hipLaunchKernelGGL((k_norm_grad_sums<T, S, ACT, ONE>), dim3(work), dim3(p.threads), lds_bytes(p, 64, 0, false) + 32 * p.nv, st, a, p);
+    if (work + params)
+        hipLaunchKernelGGL((k_norm_grad_apply<T, S, ACT, ONE>), dim3(work + params), dim3(p.threads), lds_bytes(p, 8, a.groups, false),
+                           st, a, p, params);
+}
+
+template <uint32_t T, uint32_t S, uint32_t ACT>
+void backward_act(const NormArgs &a, hipStream_t st)
+{
+    if (a.channels / a.groups % 8 == 0) backward_as<T, S, ACT, true>(a, st);
+    else backward_as<T, S, ACT, false>(a, st);
 }
 
 template <uint32_t T, uint32_t S>
-void backward_as(const NormArgs &a, hipStream_t st)
+void backward_from(const NormArgs &a, hipStream_t st)
 {
-    const Plan p = make_plan(a, 1);
-    const uint32_t work = a.spatial ? (uint32_t)(a.batch * p.chunks) : 0;
-    const uint32_t params = a.dgamma || a.dbeta ? (a.channels + 15) / 16 : 0;
-    if (work) hipLaunchKernelGGL((k_norm_grad_sums<T, S>), dim3(work), dim3(p.threads), lds_bytes(a, p, 32), st, a, p);
-    if (work + params)
-        hipLaunchKernelGGL((k_norm_grad_apply<T, S>), dim3(work + params), dim3(p.threads), lds_bytes(a, p, 8), st, a, p, params);
+    if (a.act == kActSilu) backward_act<T, S, kActSilu>(a, st);
+    else if (a.act == kActRelu) backward_act<T, S, kActRelu>(a, st);
+    else backward_act<T, S, kActNone>(a, st);
 }
 
 template <uint32_t T>
 void backward_of(const NormArgs &a, hipStream_t st)
 {
-    if (!a.codes) backward_as<T, kPlain>(a, st);
-    else if (a.format == kByteInt8) backward_as<T, kByteInt8>(a, st);
-    else backward_as<T, kByteE4M3>(a, st);
+    if (!a.codes) backward_from<T, kPlain>(a, st);
+    else if (a.format == kByteInt8) backward_from<T, kByteInt8>(a, st);
+    else backward_from<T, kByteE4M3>(a, st);
+}
+
+template <uint32_t T, bool EVEN>
+void forward_to(const NormArgs &a, hipStream_t st)
+{
+    if (!a.codes) forward_as<T, kPlain, EVEN>(a, st);
+    else if (a.format == kByteInt8) forward_as<T, kByteInt8, EVEN>(a, st);
+    else forward_as<T, kByteE4M3, EVEN>(a, st);
+}
+
+template <uint32_t T>
+void forward_of(const NormArgs &a, hipStream_t st)
+{
+    if (a.channels % 8 == 0) forward_to<T, true>(a, st);
+    else forward_to<T, false>(a, st);
 }
 
 }  // namespace
@@ -417,9 +879,9 @@ void backward_of(const NormArgs &a, hipStream_t st)
 // position takes).
 uint64_t group_norm_work(const NormArgs &a)
 {
-    uint64_t most = 0;
+    uint64_t most = 8ull * a.batch * a.channels;                          // sums of every sample, per channel
     for (uint32_t lanes : {1u, 4u, 8u, 16u}) {
-        const uint64_t records = a.batch * make_plan(a, lanes).chunks;
+        const uint64_t records = a.batch * two_pass_plan(a, lanes).chunks;
         const uint64_t bytes = records * (16ull * a.groups + (lanes == 1u ? 8ull * a.channels : 0ull));
         if (bytes > most) most = bytes;
     }
@@ -428,9 +890,9 @@ uint64_t group_norm_work(const NormArgs &a)
 
 void launch_group_norm(const NormArgs &a, hipStream_t st)
 {
-    if (a.type == kTypeF32) forward_as<kTypeF32>(a, st);
-    else if (a.type == kTypeF16) forward_as<kTypeF16>(a, st);
-    else forward_as<kTypeBF16>(a, st);
+    if (a.type == kTypeF32) forward_of<kTypeF32>(a, st);
+    else if (a.type == kTypeF16) forward_of<kTypeF16>(a, st);
+    else forward_of<kTypeBF16>(a, st);
 }
 
 void launch_group_norm_grad(const NormArgs &a, hipStream_t st)
