@@ -6,6 +6,7 @@
 // or three bf16 terms that add up to the value exactly, at two or three times the matrix work.
 #include "cmpz_byte.h"
 
+#include <cmath>
 #include <type_traits>
 
 namespace cmpz {
@@ -462,81 +463,154 @@ __global__ __launch_bounds__(kThreads) void k_linear_grad_few(LinearGradArgs a, 
     }
 }
 
-// Joins the partial sums of the ranges of rows, in their order; dW's if there are several, db's.
-__global__ __launch_bounds__(kThreads) void k_linear_grad_join(LinearGradArgs a, uint32_t splits, uint32_t splits_b, uint64_t values)
+// Joins the partial sums of the ranges of rows: `count` rows of `n` values each to one row of results.  A thread takes four
+// values (one where rows are not multiples of four) of every PARTS-th row, then the PARTS sums are added up in
+// order: with many ranges and few results there would be too few loads in flight otherwise.
+template <uint32_t PARTS>
+__global__ __launch_bounds__(kThreads) void k_linear_grad_join(const float *w, uint32_t count, uint64_t n, void *out, uint32_t type,
+                                                               uint32_t accumulate)
 {
-    const uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
-    const uint64_t first = splits > 1 ? values : 0;                       // work items of dW, before those of db
-    if (i < first) {
-        float s = 0.0f;
-        for (uint32_t k = 0; k < splits; ++k) s += a.work[(uint64_t)k * values + i];
-        put(a.dw, i, a.out_type, s, a.accumulate);
-    } else if (a.db && splits_b > 1 && i - first < a.outs) {
-        const float *w = a.work + (uint64_t)(splits > 1 ? splits : 0) * values + (i - first);
-        float s = 0.0f;
-        for (uint32_t k = 0; k < splits_b; ++k) s += w[(uint64_t)k * a.outs];
-        put(a.db, i - first, a.out_type, s, a.accumulate);
+    __shared__ f32x4 s[PARTS > 1 ? kThreads : 1];
+    const uint32_t part = threadIdx.x % PARTS, slot = threadIdx.x / PARTS;
+    const uint64_t i = ((uint64_t)blockIdx.x * (kThreads / PARTS) + slot) * 4u;
+    const int left = i < n ? (n - i < 4 ? (int)(n - i) : 4) : 0;
+    f32x4 t = {0, 0, 0, 0};
+    if (left == 4) {
+#pragma unroll 4
+        for (uint32_t k = part; k < count; k += PARTS) {
+            f32x4 v;
+            __builtin_memcpy(&v, w + k * n + i, 16);
+            t += v;
+        }
+    } else {
+        for (uint32_t k = part; k < count; k += PARTS)
+            for (int q = 0; q < 4; ++q)
+                if (q < left) t[q] += w[k * n + i + q];
     }
+    if constexpr (PARTS > 1) {
+        s[threadIdx.x] = t;
+        __syncthreads();
+        if (part) return;
+        for (uint32_t k = 1; k < PARTS; ++k) t += s[threadIdx.x + k];
+    }
+    if (left > 0) put4(out, i, type, t, accumulate, left);
 }
 
-constexpr uint32_t kTileN = 256, kTileK = 256;
+void launch_join(const float *w, uint32_t count, uint64_t n, void *out, uint32_t type, uint32_t accumulate, hipStream_t st)
+{
+    const uint32_t parts = count >= 32 ? 16 : count >= 8 ? 4 : 1;
+    const dim3 grid((uint32_t)((n + 4 * (kThreads / parts) - 1) / (4 * (kThreads / parts)))), block(kThreads);
+    if (parts == 16) hipLaunchKernelGGL(k_linear_grad_join<16>, grid, block, 0, st, w, count, n, out, type, accumulate);
+    else if (parts == 4) hipLaunchKernelGGL(k_linear_grad_join<4>, grid, block, 0, st, w, count, n, out, type, accumulate);
+    else hipLaunchKernelGGL(k_linear_grad_join<1>, grid, block, 0, st, w, count, n, out, type, accumulate);
+}
+
+// Tiles of dW that a workgroup may take, and what a stage of one costs a CU in clock cycles: the matrix units do 4096
+// operations a cycle, LDS moves 128 bytes; `floor`: a stage of a workgroup that has the CU to itself takes as
+// long, whatever its size (barrier, LDS and load latencies).
+struct Tile { uint32_t n, k, resident; };
+constexpr Tile kTiles[] = {{256, 256, 1}, {128, 128, 2}, {64, 256, 2}, {64, 64, 4}};
+constexpr int kTileCount = 4, kFewOutputs = kTileCount;
 
 bool few_outputs(uint64_t cols, uint64_t outs) { return outs < 8 || cols == 0; }
 
-Plan make_plan(uint64_t rows, uint64_t cols, uint64_t outs)
+// Time of a launch in clock cycles, roughly: what the choice between tiles and numbers of ranges goes by.
+double cost_of(const Tile &t, uint64_t rows, uint64_t cols, uint64_t outs, uint32_t type, uint64_t splits)
 {
-    Plan p;
-    const bool few = few_outputs(cols, outs);
-    const uint32_t tile_n = few ? 8 : kTileN, tile_k = few ? 4 * kThreads : kTileK;
+    const double terms = type == kTypeBF16 ? 1 : type == kTypeF16 ? 2 : 3;
+    const double groups = (double)((outs + t.n - 1) / t.n) * (double)((cols + t.k - 1) / t.k) * (double)splits;
+    const double stages = std::ceil((double)rows / kStep / (double)splits) + 3;        // and what a workgroup begins with
+    const double matrix = 2.0 * t.n * t.k * kStep * terms / 4096.0;
+    const double lds = (2.0 * 64 * (t.n * terms + t.k) + 64.0 * (t.n * terms + t.k)) / 128.0;
+    const double work = matrix > lds ? matrix : lds, floor_ = 700;
+    const double per_cu = std::ceil(groups / 256.0);
+    const double rounds = std::ceil(per_cu / t.resident), at_once = per_cu < t.resident ? per_cu : t.resident;
+    const double stage = work * at_once > floor_ ? work * at_once : floor_;
+    const double results = (double)t.n * t.k * (splits > 1 ? 4 : 2) * per_cu / 16.0;
+    const double memory = (double)rows * ((double)outs * type_bytes(type) + (double)cols) / 2000.0;  // 5 TB/s at 2.4 GHz
+    const double body = rounds * stages * stage;
+    return (body > memory ? body : memory) + results + (splits > 1 ? 8000.0 + (double)splits * outs * cols * 8.0 / 2000.0 : 0.0);
+}
+
+struct Choice { int tile; Plan plan; };
+
+Choice choose(uint64_t rows, uint64_t cols, uint64_t outs, uint32_t type)
+{
+    const uint64_t steps = (rows + kStep - 1) / kStep;
+    Choice c{kFewOutputs, {}};
+    uint64_t splits = 1;
+    uint32_t tile_n = 8, tile_k = 4 * kThreads;
+    if (few_outputs(cols, outs)) {
+        const uint64_t tiles = ((outs + 7) / 8) * ((cols + tile_k - 1) / tile_k + (cols == 0));
+        splits = tiles && tiles < 1024 ? 1024 / tiles : 1;
+        if (splits > (steps + 1) / 2) splits = (steps + 1) / 2;           // no fewer than two stages each
+    } else {
+        double best = 0;
+        for (int i = 0; i < kTileCount; ++i) {
+            const uint64_t tiles = ((outs + kTiles[i].n - 1) / kTiles[i].n) * ((cols + kTiles[i].k - 1) / kTiles[i].k);
+            // one range, and as many as fill a quarter of the CUs, half of them, all of them once, twice, ...
+            for (uint64_t fill : {0ull, 64ull, 128ull, 256ull, 512ull, 768ull, 1024ull}) {
+                uint64_t k = fill / tiles;
+                if (fill && (k < 2 || fill > 256ull * kTiles[i].resident)) continue;
+                if (k > steps / 4) k = steps / 4;                         // no fewer than four stages each
+                if (k < 1) k = 1;
+                const double t = cost_of(kTiles[i], rows, cols, outs, type, k);
+                if (best == 0 || t < best) { best = t; c.tile = i; splits = k; }
+            }
+        }
+        tile_n = kTiles[c.tile].n;
+        tile_k = kTiles[c.tile].k;
+    }
+    if (splits < 1) splits = 1;
+    Plan &p = c.plan;
     p.tiles_n = outs ? (uint32_t)((outs + tile_n - 1) / tile_n) : 1;
     p.tiles_k = cols ? (uint32_t)((cols + tile_k - 1) / tile_k) : 1;       // without columns the bias gradient is left
-    const uint64_t tiles = (uint64_t)p.tiles_n * p.tiles_k, want = few ? 1024 : 256;
-    uint64_t splits = tiles >= want ? 1 : want / tiles;
-    const uint64_t steps = (rows + kStep - 1) / kStep, least = few ? 2 : 8;
-    if (splits > (steps + least - 1) / least) splits = (steps + least - 1) / least;
-    if (splits < 1) splits = 1;
-    p.rows_per = (uint32_t)((steps + splits - 1) / splits * kStep);
-    if (p.rows_per == 0) p.rows_per = kStep;
-    p.splits = (uint32_t)((rows + p.rows_per - 1) / p.rows_per);
-    if (p.splits < 1) p.splits = 1;
-    p.parts_b = few ? p.splits : p.splits * p.tiles_k;
-    return p;
+    p.rows_per = steps ? (uint32_t)((steps + splits - 1) / splits * kStep) : kStep;
+    p.splits = rows ? (uint32_t)((rows + p.rows_per - 1) / p.rows_per) : 1;
+    p.parts_b = c.tile == kFewOutputs ? p.splits : p.splits * p.tiles_k;
+    return c;
 }
 
 template <uint32_t T, uint32_t F>
-void launch_as(const LinearGradArgs &a, const Plan &p, hipStream_t st)
+void launch_as(const LinearGradArgs &a, const Choice &c, hipStream_t st)
 {
+    const Plan &p = c.plan;
     const dim3 grid(p.tiles_n * p.tiles_k * p.splits), block(kThreads);
-    if (few_outputs(a.cols, a.outs)) hipLaunchKernelGGL((k_linear_grad_few<T, F>), grid, block, 0, st, a, p);
-    else hipLaunchKernelGGL((k_linear_grad<T, F, 4, 4, 2, 2>), grid, block, 0, st, a, p);
+    switch (c.tile) {
+    case 0: hipLaunchKernelGGL((k_linear_grad<T, F, 4, 4, 2, 2>), grid, block, 0, st, a, p); break;
+    case 1: hipLaunchKernelGGL((k_linear_grad<T, F, 2, 2, 2, 2>), grid, block, 0, st, a, p); break;
+    case 2: hipLaunchKernelGGL((k_linear_grad<T, F, 2, 2, 1, 4>), grid, block, 0, st, a, p); break;
+    case 3: hipLaunchKernelGGL((k_linear_grad<T, F, 1, 1, 2, 2>), grid, block, 0, st, a, p); break;
+    default: hipLaunchKernelGGL((k_linear_grad_few<T, F>), grid, block, 0, st, a, p);
+    }
 }
 
 template <uint32_t T>
-void launch_of(const LinearGradArgs &a, const Plan &p, hipStream_t st)
+void launch_of(const LinearGradArgs &a, const Choice &c, hipStream_t st)
 {
-    if (a.format == kByteInt8) launch_as<T, kByteInt8>(a, p, st);
-    else launch_as<T, kByteE4M3>(a, p, st);
+    if (a.format == kByteInt8) launch_as<T, kByteInt8>(a, c, st);
+    else launch_as<T, kByteE4M3>(a, c, st);
 }
 
 }  // namespace
 
 uint64_t linear_grad_work(uint64_t rows, uint64_t cols, uint64_t outs, uint32_t type)
 {
-    const Plan p = make_plan(rows, cols, outs);
+    const Plan p = choose(rows, cols, outs, type).plan;
     return 4ull * ((p.splits > 1 ? p.splits * outs * cols : 0) + (p.parts_b > 1 ? p.parts_b * outs : 0));
 }
 
 void launch_linear_grad(const LinearGradArgs &a, hipStream_t st)
 {
-    const Plan p = make_plan(a.rows, a.cols, a.outs);
-    if (a.type == kTypeF32) launch_of<kTypeF32>(a, p, st);
-    else if (a.type == kTypeF16) launch_of<kTypeF16>(a, p, st);
-    else launch_of<kTypeBF16>(a, p, st);
+    const Choice c = choose(a.rows, a.cols, a.outs, a.type);
+    const Plan &p = c.plan;
+    if (a.type == kTypeF32) launch_of<kTypeF32>(a, c, st);
+    else if (a.type == kTypeF16) launch_of<kTypeF16>(a, c, st);
+    else launch_of<kTypeBF16>(a, c, st);
     const uint64_t values = (uint64_t)a.outs * a.cols;
-    const uint64_t items = (p.splits > 1 ? values : 0) + (a.db && p.parts_b > 1 ? a.outs : 0);
-    if (items)
-        hipLaunchKernelGGL(k_linear_grad_join, dim3((uint32_t)((items + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, a, p.splits,
-                           p.parts_b, values);
+    if (p.splits > 1 && values) launch_join(a.work, p.splits, values, a.dw, a.out_type, a.accumulate, st);
+    if (a.db && p.parts_b > 1)
+        launch_join(a.work + (p.splits > 1 ? p.splits * values : 0), p.parts_b, a.outs, a.db, a.out_type, a.accumulate, st);
 }
 
 }  // namespace cmpz
