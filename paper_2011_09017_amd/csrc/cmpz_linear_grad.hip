@@ -20,7 +20,8 @@ typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
 
 constexpr uint32_t kStep = 32;                 // rows of a stage: the reduction of one matrix instruction
 constexpr uint32_t kThreads = 256;             // four waves
-constexpr uint32_t kPad = 32;                  // behind a row in LDS: the four rows of a transposed read lie in different banks
+constexpr uint32_t kPad = 64;                  // behind a row in LDS: the four rows of a transposed read of 32 columns lie in
+                                               // different banks
 
 template <uint32_t T> constexpr int kTerms = T == kTypeBF16 ? 1 : T == kTypeF16 ? 2 : 3;
 
@@ -149,14 +150,16 @@ __device__ __forceinline__ f32x8 values_of(const Raw<T> &r)
     return v;
 }
 
-// A workgroup computes TN x TK results over a range of rows, 32 rows (a stage) at a time.  Four waves, WN x WK of them, take
-// FN x FK results of 32 x 32 each.  Two stages lie in LDS.  While the matrix units work on the operands of stage t, which
-// are in registers, a wave reads those of stage t + 1, stores stage t + 2 over stage t (which every wave has read
-// when it passes the one barrier of the stage) and loads stage t + 4 from memory.  The number of stages is even, so that
-// registers and LDS slots alternate by a compile-time index; rows of zeros before the first fill the first two.
+// A workgroup computes TN x TK results over a range of rows, 32 rows (a stage) at a time.  WN x WK waves take FN x FK
+// results of 32 x 32 each.  Two stages lie in LDS.  A stage is worked on in units: 16 of its rows, one term of dY.  While
+// the matrix units work on the operands of one unit, which are in registers, a wave reads those of the next; in the last
+// unit of stage t it also stores stage t + 2 over stage t (which every wave has read when it passes the one barrier
+// of the stage) and loads stage t + 4 from memory.  The number of stages is even, so that the registers of the loads and
+// the LDS slots alternate by a compile-time index; rows of zeros before the first fill the first two.
 template <uint32_t T, uint32_t F, int FN, int FK, int WN, int WK>
-__global__ __launch_bounds__(kThreads, FN * FK > 4 ? 1 : 2) void k_linear_grad(LinearGradArgs a, Plan p)
+__global__ __launch_bounds__(64 * WN * WK, 2) void k_linear_grad(LinearGradArgs a, Plan p)
 {
+    constexpr uint32_t kThreads = 64 * WN * WK;
     constexpr int TERMS = kTerms<T>;
     constexpr uint32_t ES = type_bytes(T);
     constexpr uint32_t TN = FN * 32 * WN, TK = FK * 32 * WK;
@@ -164,10 +167,10 @@ __global__ __launch_bounds__(kThreads, FN * FK > 4 ? 1 : 2) void k_linear_grad(L
     constexpr uint32_t VY = TN / 8, VX = TK / 16;                         // vectors of a row
     constexpr uint32_t YV = VY * kStep / kThreads, XV = VX * kStep >= kThreads ? VX * kStep / kThreads : 1;
     constexpr uint32_t RY = kThreads / VY, RX = kThreads / VX;            // rows between a thread's vectors
-    static_assert(WN * WK == 4 && YV >= 1, "four waves");
+    static_assert(YV >= 1, "every thread brings a part of dY");
     // one block of LDS: two stages of dY's terms, two of x', and at the end the rows of the results
     constexpr uint32_t SY = kStep * PY, SX = kStep * PX, RW = FK * 32 + 4, RV = FK * 8;
-    constexpr uint32_t kStages = 2 * TERMS * SY + 2 * SX, kRows = 4 * 32 * RW * 4;
+    constexpr uint32_t kStages = 2 * TERMS * SY + 2 * SX, kRows = WN * WK * 32 * RW * 4;
     __shared__ __align__(16) uint8_t s_all[kStages > kRows ? kStages : kRows];
     auto s_y = [&](int slot, int term) -> uint8_t * { return s_all + (slot * TERMS + term) * SY; };
     auto s_x = [&](int slot) -> uint8_t * { return s_all + 2 * TERMS * SY + slot * SX; };
@@ -205,7 +208,6 @@ __global__ __launch_bounds__(kThreads, FN * FK > 4 ? 1 : 2) void k_linear_grad(L
     }
     struct Fetched { Raw<T> y[YV]; u32x4 x[XV]; uint32_t e[XV]; } got[2];
     auto load = [&](Fetched &g, uint32_t s) {                             // stage 2 or later: all its rows exist
-        if (s >= stages) return;
         const uint64_t m0 = (uint64_t)(m_zero + (int64_t)s * kStep);
         const uint8_t *y = dy + m0 * row_y, *x = a.codes + m0 * a.pitch, *e = a.exps + m0 * a.ngroups;
 #pragma unroll
@@ -299,60 +301,69 @@ __global__ __launch_bounds__(kThreads, FN * FK > 4 ? 1 : 2) void k_linear_grad(L
     for (int i = 0; i < FK; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x16{};
-    bf16x8 fy[2][2][FN], fx[2][2][FK];                                    // [buffer][half of the stage]
-    auto read_y = [&](bf16x8 (&f)[2][FN], int slot, int term) {
+    bf16x8 fy[2][FN], fx[2][FK];
+    auto read_y = [&](int buffer, int slot, int term, int half) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < FN; ++j) f[h][j] = transposed<PY>(s_y(slot, term) + at_y + h * 16u * PY + 64u * j);
+        for (int j = 0; j < FN; ++j) fy[buffer][j] = transposed<PY>(s_y(slot, term) + at_y + half * 16u * PY + 64u * j);
     };
-    auto read_x = [&](bf16x8 (&f)[2][FK], int slot) {
+    auto read_x = [&](int slot, int half) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < FK; ++i) f[h][i] = transposed<PX>(s_x(slot) + at_x + h * 16u * PX + 64u * i);
+        for (int i = 0; i < FK; ++i) fx[half][i] = transposed<PX>(s_x(slot) + at_x + half * 16u * PX + 64u * i);
     };
-    auto multiply = [&](const bf16x8 (&x)[FK], const bf16x8 (&y)[FN]) {
+    auto multiply = [&](int half, int buffer) {
 #pragma unroll
         for (int i = 0; i < FK; ++i)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < FN; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[half][i], fy[buffer][j], acc[i][j], 0, 0, 0);
     };
 
-    auto step = [&](auto parity, uint32_t t) {
+    // bf16: one region of the last half of stage t and the first of stage t + 1, all of whose operands it reads, so that
+    // the expansion can lie between any of its products.  With several terms the split is spread better by the
+    // units, one after the other; the barrier stands before the last.
+    auto step = [&](auto parity, auto more, auto last, uint32_t t) {
         constexpr int P = decltype(parity)::value;
+        constexpr int UNITS = 2 * TERMS;                                  // unit u: half u / TERMS, term u % TERMS
+        uint32_t found = 0;
+        // behind the barrier every wave has the operands of stage t in registers, and stage t + 1 is stored
+        if constexpr (TERMS == 1) {
+            __syncthreads();
+            read_y(0, P ^ 1, 0, 0);
+            read_x(P ^ 1, 0);
+            found = store(got[P], P);
+            multiply(1, 1);
+            read_y(1, P ^ 1, 0, 1);
+            read_x(P ^ 1, 1);
+            if constexpr (!decltype(last)::value) multiply(0, 0);
 #pragma unroll
-        for (int u = 0; u + 1 < TERMS; ++u) {
-            const int now = (P * TERMS + u) & 1;
-            read_y(fy[now ^ 1], P, u + 1);
-            multiply(fx[P][0], fy[now][0]);
-            multiply(fx[P][1], fy[now][1]);
-        }
-        constexpr int now = (P * TERMS + TERMS - 1) & 1;
-        // every wave has the last operands of stage t in registers, and stage t + 1 is stored
-        __syncthreads();
-        read_y(fy[now ^ 1], P ^ 1, 0);
-        read_x(fx[P ^ 1], P ^ 1);
-        multiply(fx[P][0], fy[now][0]);
-        // reads between the first half's products, the expansion and its stores between the second half's
+            for (int k = 0; k < 2 * FN * FK; ++k) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);        // a matrix instruction
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);        // LDS reads
+                __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);        // vector arithmetic
+                if (k & 1) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);   // an LDS write
+            }
+        } else {
 #pragma unroll
-        for (int k = 0; k < FN * FK; ++k) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);            // matrix
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);            // LDS reads
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        const uint32_t found = store(got[P], P);
-        multiply(fx[P][1], fy[now][1]);
+            for (int u = 0; u < UNITS; ++u) {
+                const int next = (u + 1) % UNITS, slot = u + 1 < UNITS ? P : P ^ 1;
+                if (u + 1 == UNITS) __syncthreads();
+                read_y(next & 1, slot, next % TERMS, next / TERMS);
+                if (next % TERMS == 0) read_x(slot, next / TERMS);
+                if (u + 1 == UNITS) found = store(got[P], P);
+                multiply(u / TERMS, u & 1);
 #pragma unroll
-        for (int k = 0; k < FN * FK; ++k) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
-            __builtin_amdgcn_sched_group_barrier(0x002, 6, 1);            // vector arithmetic
-            if (k & 1) __builtin_amdgcn_sched_group_barrier(0x200, 1, 1); // LDS writes
+                for (int k = 0; k < FN * FK; ++k) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 8, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         __builtin_amdgcn_sched_barrier(0);
         if (F == kByteInt8 && (found & 0x80808080u)) mark_nan(got[P], P);
         sum_bias(got[P], t + 2);
-        load(got[P], t + 4);
+        if constexpr (decltype(more)::value) load(got[P], t + 4);
     };
 
     if (stages > 0) {
@@ -361,16 +372,36 @@ __global__ __launch_bounds__(kThreads, FN * FK > 4 ? 1 : 2) void k_linear_grad(L
             load_first(got[s], s);
             if (store(got[s], s) & 0x80808080u) mark_nan(got[s], s);
             sum_bias(got[s], s);
-            load(got[s], s + 2);
+            if (stages > 2) load(got[s], s + 2);
         }
         __syncthreads();
-        read_y(fy[0], 0, 0);
-        read_x(fx[0], 0);
+        read_y(0, 0, 0, 0);
+        read_x(0, 0);
+        if constexpr (TERMS == 1) {                                       // stage 0 but its last unit
+            multiply(0, 0);
+            read_y(1, 0, 0, 1);
+            read_x(0, 1);
+        }
     }
+    // The loads of the loop are unconditional: behind a branch the wait for a stage would be one for all loads under way.
+    const std::integral_constant<int, 0> even;
+    const std::integral_constant<int, 1> odd;
+    const std::true_type yes;
+    const std::false_type no;
+    uint32_t t = 0;
 #pragma unroll 1
-    for (uint32_t t = 0; t < stages; t += 2) {
-        step(std::integral_constant<int, 0>{}, t);
-        step(std::integral_constant<int, 1>{}, t + 1);
+    for (; t + 4 < stages; t += 2) {
+        step(even, yes, no, t);
+        step(odd, yes, no, t + 1);
+    }
+    if (t + 2 < stages) {
+        step(even, no, no, t);
+        step(odd, no, no, t + 1);
+        t += 2;
+    }
+    if (t < stages) {
+        step(even, no, no, t);
+        step(odd, no, yes, t + 1);
     }
 
     // ---- results: a lane holds column n = lane % 16 and four consecutive k of every 16 x 16; sixteen rows of dW at a
@@ -505,31 +536,30 @@ void launch_join(const float *w, uint32_t count, uint64_t n, void *out, uint32_t
     else hipLaunchKernelGGL(k_linear_grad_join<1>, grid, block, 0, st, w, count, n, out, type, accumulate);
 }
 
-// Tiles of dW that a workgroup may take, and what a stage of one costs a CU in clock cycles: the matrix units do 4096
-// operations a cycle, LDS moves 128 bytes; `floor`: a stage of a workgroup that has the CU to itself takes as
-// long, whatever its size (barrier, LDS and load latencies).
-struct Tile { uint32_t n, k, resident; };
-constexpr Tile kTiles[] = {{256, 256, 1}, {128, 128, 2}, {64, 256, 2}, {64, 64, 4}};
+// Tiles of dW that a workgroup may take, how many such workgroups a CU holds, and what a stage takes with w of them on
+// it, in ns, for t terms: a0 + a1 * t + (b0 + b1 * t) * w.  Fitted to 8192 rows, one to four workgroups per CU and one to three
+// terms (ns measured / fitted at w = 1, 2; bf16): 256 x 256: 1190 / 1170; 128 x 128: 539, 780 / 539, 780; 64 x 256: 699, 986 /
+// 700, 985; 64 x 64: 428, 542 / 431, 564; fp32: 2550 / 2550; 1251, 1798 / 1251, 1798; 1219, 1759 / 1220, 1755; 727, 950 / 733, 1032.
+struct Tile { uint32_t n, k, resident; double a0, a1, b0, b1; };
+constexpr Tile kTiles[] = {{256, 256, 1, 480, 690, 0, 0}, {128, 128, 2, 95, 203, 88, 153}, {64, 256, 2, 280, 135, 160, 125},
+                           {64, 64, 4, 230, 68, 50, 83}};
 constexpr int kTileCount = 4, kFewOutputs = kTileCount;
 
 bool few_outputs(uint64_t cols, uint64_t outs) { return outs < 8 || cols == 0; }
 
-// Time of a launch in clock cycles, roughly: what the choice between tiles and numbers of ranges goes by.
+// Time of the launches in ns, roughly: what the choice between tiles and numbers of ranges goes by.
 double cost_of(const Tile &t, uint64_t rows, uint64_t cols, uint64_t outs, uint32_t type, uint64_t splits)
 {
     const double terms = type == kTypeBF16 ? 1 : type == kTypeF16 ? 2 : 3;
-    const double groups = (double)((outs + t.n - 1) / t.n) * (double)((cols + t.k - 1) / t.k) * (double)splits;
+    const double tiles = (double)((outs + t.n - 1) / t.n) * (double)((cols + t.k - 1) / t.k);
+    const double per_cu = std::ceil(tiles * (double)splits / 256.0);
+    const double full = std::floor(per_cu / t.resident), rest = per_cu - full * t.resident;
+    auto stage = [&](double w) { return w > 0 ? t.a0 + t.a1 * terms + (t.b0 + t.b1 * terms) * w : 0.0; };
     const double stages = std::ceil((double)rows / kStep / (double)splits) + 3;        // and what a workgroup begins with
-    const double matrix = 2.0 * t.n * t.k * kStep * terms / 4096.0;
-    const double lds = (2.0 * 64 * (t.n * terms + t.k) + 64.0 * (t.n * terms + t.k)) / 128.0;
-    const double work = matrix > lds ? matrix : lds, floor_ = 700;
-    const double per_cu = std::ceil(groups / 256.0);
-    const double rounds = std::ceil(per_cu / t.resident), at_once = per_cu < t.resident ? per_cu : t.resident;
-    const double stage = work * at_once > floor_ ? work * at_once : floor_;
-    const double results = (double)t.n * t.k * (splits > 1 ? 4 : 2) * per_cu / 16.0;
-    const double memory = (double)rows * ((double)outs * type_bytes(type) + (double)cols) / 2000.0;  // 5 TB/s at 2.4 GHz
-    const double body = rounds * stages * stage;
-    return (body > memory ? body : memory) + results + (splits > 1 ? 8000.0 + (double)splits * outs * cols * 8.0 / 2000.0 : 0.0);
+    const double body = stages * (full * stage(t.resident) + stage(rest));
+    const double memory = (double)rows * ((double)outs * type_bytes(type) + (double)cols) / 5000.0;    // at 5 TB/s
+    const double results = (double)t.n * t.k * (splits > 1 ? 4 : 2) * per_cu / 40.0;                   // stores at 40 B/ns per CU
+    return (body > memory ? body : memory) + results + (splits > 1 ? 3000.0 + (double)splits * outs * cols * 4.0 / 5000.0 : 0.0);
 }
 
 struct Choice { int tile; Plan plan; };
@@ -577,7 +607,7 @@ void launch_as(const LinearGradArgs &a, const Choice &c, hipStream_t st)
     const Plan &p = c.plan;
     const dim3 grid(p.tiles_n * p.tiles_k * p.splits), block(kThreads);
     switch (c.tile) {
-    case 0: hipLaunchKernelGGL((k_linear_grad<T, F, 4, 4, 2, 2>), grid, block, 0, st, a, p); break;
+    case 0: hipLaunchKernelGGL((k_linear_grad<T, F, 4, 2, 2, 4>), grid, dim3(512), 0, st, a, p); break;
     case 1: hipLaunchKernelGGL((k_linear_grad<T, F, 2, 2, 2, 2>), grid, block, 0, st, a, p); break;
     case 2: hipLaunchKernelGGL((k_linear_grad<T, F, 2, 2, 1, 4>), grid, block, 0, st, a, p); break;
     case 3: hipLaunchKernelGGL((k_linear_grad<T, F, 1, 1, 2, 2>), grid, block, 0, st, a, p); break;
