@@ -16,12 +16,14 @@ struct DeviceGuard {
     int rc = CMP_OK;
     explicit DeviceGuard(int dev)
     {
-        int n = 0;
-        if (hipGetDeviceCount(&n) != hipSuccess) { rc = CMP_E_HIP; return; }
-        if (dev < 0 || dev >= n) { rc = CMP_E_ARG; return; }
+        if (dev < 0) { rc = CMP_E_ARG; return; }
         if (hipGetDevice(&prev) != hipSuccess) { prev = -1; rc = CMP_E_HIP; return; }
-        if (prev == dev) prev = -1;
-        else if (hipSetDevice(dev) != hipSuccess) rc = CMP_E_HIP;
+        if (prev == dev) { prev = -1; return; }
+        const hipError_t e = hipSetDevice(dev);
+        if (e == hipSuccess) return;
+        (void)hipGetLastError();                                          // it would come back from the next call that asks
+        rc = e == hipErrorInvalidDevice ? CMP_E_ARG : CMP_E_HIP;
+        prev = -1;
     }
     ~DeviceGuard() { if (prev >= 0) (void)hipSetDevice(prev); }
 };

@@ -494,46 +494,48 @@ __global__ __launch_bounds__(kThreads) void k_linear_grad_few(LinearGradArgs a, 
     }
 }
 
-// Joins the partial sums of the ranges of rows: `count` rows of `n` values each to one row of results.  A thread takes four
-// values (one where rows are not multiples of four) of every PARTS-th row, then the PARTS sums are added up in
-// order: with many ranges and few results there would be too few loads in flight otherwise.
-template <uint32_t PARTS>
-__global__ __launch_bounds__(kThreads) void k_linear_grad_join(const float *w, uint32_t count, uint64_t n, void *out, uint32_t type,
-                                                               uint32_t accumulate)
+// Joins the partial sums of the ranges of rows: `count` rows of `n` values each to one row of results, dW's and db's in one
+// launch.  A thread takes four values of every parts-th row, then the sums of the parts are added up in order: with
+// many ranges and few results there would be too few loads in flight otherwise.
+struct JoinJob { const float *w; void *out; uint64_t n; uint32_t count, parts_log, blocks; };
+
+__global__ __launch_bounds__(kThreads) void k_linear_grad_join(JoinJob a, JoinJob b, uint32_t type, uint32_t accumulate)
 {
-    __shared__ f32x4 s[PARTS > 1 ? kThreads : 1];
-    const uint32_t part = threadIdx.x % PARTS, slot = threadIdx.x / PARTS;
-    const uint64_t i = ((uint64_t)blockIdx.x * (kThreads / PARTS) + slot) * 4u;
-    const int left = i < n ? (n - i < 4 ? (int)(n - i) : 4) : 0;
+    __shared__ f32x4 s[kThreads];
+    const bool first = blockIdx.x < a.blocks;
+    const JoinJob j = first ? a : b;
+    const uint32_t block = first ? blockIdx.x : blockIdx.x - a.blocks, parts = 1u << j.parts_log;
+    const uint32_t part = threadIdx.x & (parts - 1u), slot = threadIdx.x >> j.parts_log;
+    const uint64_t i = ((uint64_t)block * (kThreads >> j.parts_log) + slot) * 4u;
+    const int left = i < j.n ? (j.n - i < 4 ? (int)(j.n - i) : 4) : 0;
     f32x4 t = {0, 0, 0, 0};
     if (left == 4) {
 #pragma unroll 4
-        for (uint32_t k = part; k < count; k += PARTS) {
+        for (uint32_t k = part; k < j.count; k += parts) {
             f32x4 v;
-            __builtin_memcpy(&v, w + k * n + i, 16);
+            __builtin_memcpy(&v, j.w + k * j.n + i, 16);
             t += v;
         }
     } else {
-        for (uint32_t k = part; k < count; k += PARTS)
+        for (uint32_t k = part; k < j.count; k += parts)
             for (int q = 0; q < 4; ++q)
-                if (q < left) t[q] += w[k * n + i + q];
+                if (q < left) t[q] += j.w[k * j.n + i + q];
     }
-    if constexpr (PARTS > 1) {
+    if (parts > 1) {
         s[threadIdx.x] = t;
         __syncthreads();
         if (part) return;
-        for (uint32_t k = 1; k < PARTS; ++k) t += s[threadIdx.x + k];
+        for (uint32_t k = 1; k < parts; ++k) t += s[threadIdx.x + k];
     }
-    if (left > 0) put4(out, i, type, t, accumulate, left);
+    if (left > 0) put4(j.out, i, type, t, accumulate, left);
 }
 
-void launch_join(const float *w, uint32_t count, uint64_t n, void *out, uint32_t type, uint32_t accumulate, hipStream_t st)
+JoinJob join_job(const float *w, uint32_t count, uint64_t n, void *out)
 {
-    const uint32_t parts = count >= 32 ? 16 : count >= 8 ? 4 : 1;
-    const dim3 grid((uint32_t)((n + 4 * (kThreads / parts) - 1) / (4 * (kThreads / parts)))), block(kThreads);
-    if (parts == 16) hipLaunchKernelGGL(k_linear_grad_join<16>, grid, block, 0, st, w, count, n, out, type, accumulate);
-    else if (parts == 4) hipLaunchKernelGGL(k_linear_grad_join<4>, grid, block, 0, st, w, count, n, out, type, accumulate);
-    else hipLaunchKernelGGL(k_linear_grad_join<1>, grid, block, 0, st, w, count, n, out, type, accumulate);
+    JoinJob j{w, out, n, count, count >= 32 ? 4u : count >= 8 ? 2u : 0u, 0};
+    const uint32_t values = 4u * (kThreads >> j.parts_log);
+    j.blocks = (uint32_t)((n + values - 1) / values);
+    return j;
 }
 
 // Tiles of dW that a workgroup may take, how many such workgroups a CU holds, and what a stage takes with w of them on
@@ -638,9 +640,11 @@ void launch_linear_grad(const LinearGradArgs &a, hipStream_t st)
     else if (a.type == kTypeF16) launch_of<kTypeF16>(a, c, st);
     else launch_of<kTypeBF16>(a, c, st);
     const uint64_t values = (uint64_t)a.outs * a.cols;
-    if (p.splits > 1 && values) launch_join(a.work, p.splits, values, a.dw, a.out_type, a.accumulate, st);
-    if (a.db && p.parts_b > 1)
-        launch_join(a.work + (p.splits > 1 ? p.splits * values : 0), p.parts_b, a.outs, a.db, a.out_type, a.accumulate, st);
+    const JoinJob none{};
+    const JoinJob w = p.splits > 1 && values ? join_job(a.work, p.splits, values, a.dw) : none;
+    const JoinJob b = a.db && p.parts_b > 1 ? join_job(a.work + (p.splits > 1 ? p.splits * values : 0), p.parts_b, a.outs, a.db) : none;
+    if (w.blocks + b.blocks)
+        hipLaunchKernelGGL(k_linear_grad_join, dim3(w.blocks + b.blocks), dim3(kThreads), 0, st, w, b, a.out_type, a.accumulate);
 }
 
 }  // namespace cmpz

@@ -17,6 +17,7 @@ refuses raises :class:`.binding.CmpError`.
 from __future__ import annotations
 
 import math
+from functools import lru_cache
 from typing import NamedTuple, Optional
 
 import torch
@@ -39,12 +40,16 @@ def _type_of(t: torch.Tensor) -> int:
     return _TYPES[t.dtype]
 
 
-def _on_gpu(*tensors) -> torch.device:
-    dev = tensors[0].device
-    for t in tensors:
+def _on_gpu(first: torch.Tensor, *others) -> torch.device:
+    dev = first.device
+    for t in others:
         _refuse(t is not None and t.device != dev, "all tensors have to be on one GPU")
     _refuse(dev.type != "cuda", "tensors on a GPU are wanted (there is no CPU path)")
     return dev
+
+
+def _stream(dev: torch.device) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev.index)          # the current stream's handle, without a Stream object
 
 
 def _call(rc: int, where: str) -> None:
@@ -82,10 +87,18 @@ def _matrix(t: torch.Tensor, what: str):
     return at
 
 
-def _byte_shape(rows: int, cols: int, fmt: str, group: int) -> binding.cmp_byte_shape:
+@lru_cache(maxsize=4096)
+def _byte_shape(rows: int, cols: int, fmt: str, group: int):
+    """(the C shape, bytes of a checkpoint): depend on sizes only and are read only."""
     _refuse(fmt not in _FORMATS, f"format {fmt!r}: {' or '.join(_FORMATS)}")
     _refuse(group not in GROUPS, f"groups of {group}: 32, 64 or 128")
-    return binding.cmp_byte_shape(rows, cols, _FORMATS[fmt], group)
+    shape = binding.cmp_byte_shape(rows, cols, _FORMATS[fmt], group)
+    return shape, binding.cmp_byte_bytes(shape)
+
+
+@lru_cache(maxsize=4096)
+def _linear_work(rows: int, cols: int, fmt: str, group: int, outs: int, kind: int) -> int:
+    return binding.cmp_byte_linear_grad_work(_byte_shape(rows, cols, fmt, group)[0], outs, kind)
 
 
 class ByteCheckpoint(NamedTuple):
@@ -113,20 +126,20 @@ def _held(ck: ByteCheckpoint):
     """The C shape of a checkpoint; its buffer has to be on a GPU, dense bytes."""
     _refuse(ck.buf.dtype != torch.uint8 or not ck.buf.is_contiguous(), "checkpoint: a contiguous uint8 buffer is wanted")
     _refuse(len(ck.shape) < 1, "checkpoint: at least one dimension is wanted")
-    return _byte_shape(ck.rows, ck.cols, ck.fmt, ck.group)
+    return _byte_shape(ck.rows, ck.cols, ck.fmt, ck.group)[0]
 
 
 def byte_store(x: torch.Tensor, fmt: str = "int8", group: int = 64, out: Optional[torch.Tensor] = None) -> ByteCheckpoint:
     """Stores x (any shape, groups along the last dimension).  `out`: a uint8 buffer to store into, 16-byte aligned."""
     kind = _type_of(x)
     rows, ld = _matrix(x, "byte_store")
-    shape = _byte_shape(rows, x.shape[-1], fmt, group)
+    shape, nbytes = _byte_shape(rows, x.shape[-1], fmt, group)
     dev = _on_gpu(x, out)
     if out is None:
-        out = torch.empty(binding.cmp_byte_bytes(shape), dtype=torch.uint8, device=dev)
+        out = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     _refuse(out.dtype != torch.uint8 or not out.is_contiguous(), "byte_store: out has to be a contiguous uint8 tensor")
     _call(binding.cmp_byte_store(dev.index, shape, x.data_ptr(), kind, ld, out.data_ptr(), out.numel(),
-                                 torch.cuda.current_stream(dev).cuda_stream), "cmp_byte_store")
+                                 _stream(dev)), "cmp_byte_store")
     return ByteCheckpoint(out, tuple(x.shape), x.dtype, fmt, group)
 
 
@@ -141,7 +154,7 @@ def byte_load(ck: ByteCheckpoint, dtype: Optional[torch.dtype] = None, out: Opti
     kind = _type_of(out)
     rows, ld = _matrix(out, "byte_load")
     _call(binding.cmp_byte_load(dev.index, shape, ck.buf.data_ptr(), ck.buf.numel(), out.data_ptr(), kind, ld,
-                                torch.cuda.current_stream(dev).cuda_stream), "cmp_byte_load")
+                                _stream(dev)), "cmp_byte_load")
     return out
 
 
@@ -166,20 +179,27 @@ def byte_linear_grad(dy: torch.Tensor, ck: ByteCheckpoint, bias: bool = False, d
     _refuse(tuple(out.shape) != (outs, cols) or not out.is_contiguous(), "byte_linear_grad: out has to be contiguous, [outs, cols]")
     _refuse(out_bias is not None and (tuple(out_bias.shape) != (outs,) or not out_bias.is_contiguous() or out_bias.dtype != dtype),
             "byte_linear_grad: out_bias has to be [outs], contiguous, of out's type")
-    need = binding.cmp_byte_linear_grad_work(shape, outs, kind)
+    need = _linear_work(rows, cols, ck.fmt, ck.group, outs, kind)
     work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     _call(binding.cmp_byte_linear_grad(dev.index, shape, ck.buf.data_ptr(), ck.buf.numel(), dy.data_ptr(), kind, outs, ld,
                                        out.data_ptr(), None if out_bias is None else out_bias.data_ptr(), _TYPES[dtype],
                                        accumulate, None if work is None else work.data_ptr(), need,
-                                       torch.cuda.current_stream(dev).cuda_stream), "cmp_byte_linear_grad")
+                                       _stream(dev)), "cmp_byte_linear_grad")
     return out, out_bias
 
 
-def _norm_shape(x: torch.Tensor, groups: int, eps: float, act: str) -> binding.cmp_norm_shape:
+@lru_cache(maxsize=4096)
+def _norm_plan(batch: int, spatial: int, channels: int, groups: int, kind: int, act: str, eps: float):
+    """(the C shape, bytes of the workspace): depend on sizes only and are read only."""
+    shape = binding.cmp_norm_shape(batch, spatial, channels, groups, kind, _ACTS[act], eps)
+    return shape, binding.cmp_group_norm_work(shape)
+
+
+def _norm_shape(x: torch.Tensor, groups: int, eps: float, act: str):
     _refuse(act not in _ACTS, f"activation {act!r}: {', '.join(_ACTS)}")
     _refuse(x.dim() < 2, "group norm: [batch, ..., channels] is wanted")
     _refuse(not x.is_contiguous(), "group norm: a contiguous tensor is wanted, channels last")
-    return binding.cmp_norm_shape(x.shape[0], math.prod(x.shape[1:-1]), x.shape[-1], groups, _type_of(x), _ACTS[act], eps)
+    return _norm_plan(x.shape[0], math.prod(x.shape[1:-1]), x.shape[-1], groups, _type_of(x), act, eps)
 
 
 def _parameter(t: Optional[torch.Tensor], channels: int, what: str):
@@ -190,30 +210,24 @@ def _parameter(t: Optional[torch.Tensor], channels: int, what: str):
     return t.data_ptr()
 
 
-def _workspace(shape: binding.cmp_norm_shape, dev: torch.device):
-    need = binding.cmp_group_norm_work(shape)
-    return torch.empty(need, dtype=torch.uint8, device=dev), need
-
-
 def group_norm(x: torch.Tensor, groups: int, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
                eps: float = 1e-5, act: str = "none", save: Optional[str] = None, group: int = 64):
     """(y, stats, checkpoint) of x[batch, ..., channels]: y = act(group norm of x), act "none", "relu" or "silu"; stats is what
     :func:`group_norm_grad` needs; save="int8" or "e4m3" keeps x as a checkpoint (groups of `group` channels), else None."""
-    shape = _norm_shape(x, groups, eps, act)
+    shape, need = _norm_shape(x, groups, eps, act)
     dev = _on_gpu(x, weight, bias)
     gamma, beta = _parameter(weight, x.shape[-1], "weight"), _parameter(bias, x.shape[-1], "bias")
     y = torch.empty_like(x)
     stats = torch.empty(x.shape[0], groups, 2, dtype=torch.float64, device=dev)
     ck, fmt = None, 0
     if save is not None:
-        held = _byte_shape(shape.batch * shape.spatial, shape.channels, save, group)
+        held, nbytes = _byte_shape(shape.batch * shape.spatial, shape.channels, save, group)
         fmt = held.format
-        ck = ByteCheckpoint(torch.empty(binding.cmp_byte_bytes(held), dtype=torch.uint8, device=dev), tuple(x.shape), x.dtype,
-                            save, group)
-    work, need = _workspace(shape, dev)
+        ck = ByteCheckpoint(torch.empty(nbytes, dtype=torch.uint8, device=dev), tuple(x.shape), x.dtype, save, group)
+    work = torch.empty(need, dtype=torch.uint8, device=dev)
     _call(binding.cmp_group_norm(dev.index, shape, x.data_ptr(), gamma, beta, y.data_ptr(), stats.data_ptr(), fmt, group,
                                  None if ck is None else ck.buf.data_ptr(), 0 if ck is None else ck.buf.numel(), work.data_ptr(),
-                                 need, torch.cuda.current_stream(dev).cuda_stream), "cmp_group_norm")
+                                 need, _stream(dev)), "cmp_group_norm")
     return y, stats, ck
 
 
@@ -221,7 +235,7 @@ def group_norm_grad(dy: torch.Tensor, x, stats: torch.Tensor, groups: int, weigh
                     bias: Optional[torch.Tensor] = None, act: str = "none", params: bool = True):
     """(dx, dweight, dbias) from dy, the input (a tensor of dy's type, or its :class:`ByteCheckpoint`), and what the forward
     pass was called with and gave.  params=False: the last two are None."""
-    shape = _norm_shape(dy, groups, 1.0, act)                         # eps is in stats
+    shape, need = _norm_shape(dy, groups, 1.0, act)                   # eps is in stats
     held = isinstance(x, ByteCheckpoint)
     src = x.buf if held else x
     dev = _on_gpu(dy, src, stats, weight, bias)
@@ -237,9 +251,9 @@ def group_norm_grad(dy: torch.Tensor, x, stats: torch.Tensor, groups: int, weigh
     dweight = dbias = None
     if params:
         dweight, dbias = torch.empty(2, dy.shape[-1], dtype=torch.float32, device=dev).unbind(0)
-    work, need = _workspace(shape, dev)
+    work = torch.empty(need, dtype=torch.uint8, device=dev)
     _call(binding.cmp_group_norm_grad(dev.index, shape, dy.data_ptr(), None if held else x.data_ptr(), fmt, group,
                                       src.data_ptr() if held else None, src.numel() if held else 0, gamma, beta, stats.data_ptr(),
                                       dx.data_ptr(), dweight.data_ptr() if params else None, dbias.data_ptr() if params else None,
-                                      work.data_ptr(), need, torch.cuda.current_stream(dev).cuda_stream), "cmp_group_norm_grad")
+                                      work.data_ptr(), need, _stream(dev)), "cmp_group_norm_grad")
     return dx, dweight, dbias
