@@ -43,13 +43,15 @@ void finish_plan(Plan *p, const NormArgs &a)
     p->div_per = FastDiv::make(p->per);
 }
 
+// About 512 workgroups of 512 threads, two to a CU: each has parameters, statistics and the joining of its sums to pay for
+// (8 x 16384 x 320 bf16 forward: 60 us, with 1024 of them 68; 64 x 3136 x 256: 76 and 88; 256 x 12544 x 64: 335 and 331).
 Plan two_pass_plan(const NormArgs &a, uint32_t lanes)
 {
     Plan p{};
     p.nv = ((a.channels + 7) / 8 + lanes - 1) / lanes * lanes;
     p.rp = p.nv >= 512 ? 1 : 512 / p.nv;
     if (p.rp > a.spatial) p.rp = a.spatial ? a.spatial : 1;
-    const uint64_t want = a.batch ? (1024 + a.batch - 1) / a.batch : 1;
+    const uint64_t want = a.batch ? (512 + a.batch - 1) / a.batch : 1;
     uint64_t chunks = (a.spatial + p.rp * 4ull - 1) / (p.rp * 4ull);
     if (chunks > want) chunks = want;
     if (chunks < 1) chunks = 1;
@@ -69,8 +71,9 @@ uint32_t lcm(uint32_t x, uint32_t y)
 }
 
 // The smallest segment is a multiple of eight channels, of a group and, where codes are written, of a quantisation group
-// (or all channels).  It grows to 128 bytes of a position as long as it fits.  Small segments, down to a single wave, keep
-// all of a CU's registers busy with loads.
+// (or all channels).  It grows to 128 bytes of a position, and below that there is no slab: with 64 bytes the backward
+// pass of 128 x 784 x 512 bf16 took 192 us where two passes take 93.  Small segments, down to a single wave, keep
+// all of a CU's registers busy with loads (256 x 7 x 7 x 512 fp32, both directions: 42 us, with 1024 vectors to a segment 80).
 bool slab_plan(Plan *out, const NormArgs &a, uint32_t lanes)
 {
     if (a.spatial == 0) return false;
@@ -83,6 +86,7 @@ bool slab_plan(Plan *out, const NormArgs &a, uint32_t lanes)
     if (!fits(unit)) return false;
     p.nv = unit;
     while (p.nv + unit <= all && fits(p.nv + unit) && p.nv * 8 * type_bytes(a.type) < 128) p.nv += unit;
+    if (p.nv < all && p.nv * 8 * type_bytes(a.type) < 128) return false;
     p.chunks = (all + p.nv - 1) / p.nv;
     // Positions per thread: as many as it can hold, so that a CU has most bytes in flight; one where all threads fit the
     // chip at once and only the time of a single workgroup counts.
@@ -174,25 +178,32 @@ __device__ __forceinline__ void add_moments(f32x8 v, double (&s1)[8], double (&s
 }
 
 // Totals of the workgroup for each of `groups` groups of its segment: give(g, sum, sum of squares) by the first lane
-// of a wave.  Where a vector's channels are all of one group, they are added up before LDS.
+// of a wave.  Groups of eight channels and more: a vector lies in one or two of them, and its channels are added up to
+// these before LDS (32 bytes a thread instead of 128, which would leave a CU two workgroups).
 template <class FN>
-__device__ __forceinline__ void join_moments(double *s, double (&s1)[8], double (&s2)[8], uint32_t groups, const Plan &p, FN give)
+__device__ __forceinline__ void join_moments(double *s, double (&s1)[8], double (&s2)[8], uint32_t groups, const Plan &p, const Place &q,
+                                             uint32_t first, FN give)
 {
     const uint32_t wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63u;
-    if ((p.per & 7u) == 0) {
-        double t1 = 0.0, t2 = 0.0;
+    if (p.per >= 8) {
+        const uint32_t c0 = q.c - first, g0 = p.div_per.div(c0), cut = (g0 + 1u) * p.per - c0;   // channels in the first of the two
+        double t1 = 0.0, t2 = 0.0, u1 = 0.0, u2 = 0.0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) { t1 += s1[k]; t2 += s2[k]; }
-        s[2u * threadIdx.x] = t1;
-        s[2u * threadIdx.x + 1u] = t2;
+        for (uint32_t k = 0; k < 8; ++k) {
+            if (k < cut) { t1 += s1[k]; t2 += s2[k]; }
+            else { u1 += s1[k]; u2 += s2[k]; }
+        }
+        double *o = s + 4u * threadIdx.x;
+        o[0] = t1; o[1] = t2; o[2] = u1; o[3] = u2;
         __syncthreads();
-        const uint32_t pv = p.per / 8u, items = pv * p.rp;
         for (uint32_t g = wave; g < groups; g += waves) {
+            const uint32_t v0 = g * p.per / 8u, nv = ((g + 1u) * p.per - 1u) / 8u - v0 + 1u, items = nv * p.rp;
             t1 = t2 = 0.0;
             for (uint32_t i = lane; i < items; i += 64u) {
-                const uint32_t r = i / pv, t = r * p.nv + g * pv + (i - r * pv);
-                t1 += s[2u * t];
-                t2 += s[2u * t + 1u];
+                const uint32_t r = i / nv, v = v0 + (i - r * nv);
+                const double *in = s + 4u * (r * p.nv + v) + (8u * v < g * p.per ? 2u : 0u);
+                t1 += in[0];
+                t2 += in[1];
             }
             t1 = wave_sum(t1);
             t2 = wave_sum(t2);
@@ -311,8 +322,8 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_slab(NormArgs a, Plan p)
 #pragma unroll
     for (uint32_t i = 0; i < kSlabRows; ++i) add_moments(x[i], s1, s2);
     const uint32_t groups = (end - first) / p.per;
-    double *m = s_sum + (p.per & 7u ? 16u : 2u) * blockDim.x;
-    join_moments(s_sum, s1, s2, groups, p, [&](uint32_t g, double t1, double t2) {
+    double *m = s_sum + (p.per < 8u ? 16u : 4u) * blockDim.x;
+    join_moments(s_sum, s1, s2, groups, p, q, first, [&](uint32_t g, double t1, double t2) {
         const Moments v = moments_of(a, p, t1, t2);
         m[2 * g] = v.mean;
         m[2 * g + 1] = v.rstd;
@@ -358,38 +369,42 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_sums(NormArgs a, Plan p)
         for (; left; --left, x += step) add_moments(load8<T>(x, n), s1, s2);
     }
     double *part = static_cast<double *>(a.work);
-    join_moments(s_sum, s1, s2, a.groups, p, [&](uint32_t g, double t1, double t2) {
+    join_moments(s_sum, s1, s2, a.groups, p, q, 0, [&](uint32_t g, double t1, double t2) {
         double *o = part + (((uint64_t)q.n * a.groups + g) * p.chunks + q.chunk) * 2;
         o[0] = t1;
         o[1] = t2;
     });
 }
 
-// Two totals over the workgroups of a sample, for every group, into s[2 * g], s[2 * g + 1]: as many lanes to a group as
-// the workgroup has for all of them at once.
-__device__ __forceinline__ void join_chunks(double *s, const double *part, uint32_t n, const NormArgs &a, const Plan &p)
+// Two totals over the workgroups of a sample and group, by one wave.
+struct Totals { double t1, t2; };
+__device__ __forceinline__ Totals join_chunks(const double *part, uint64_t sample_and_group, const Plan &p)
 {
-    uint32_t lanes = 64;
-    while (lanes > 1 && a.groups * lanes > blockDim.x) lanes >>= 1;
-    const uint32_t side = blockDim.x / lanes, lane = threadIdx.x & (lanes - 1u);
-    for (uint32_t g0 = 0; g0 < a.groups; g0 += side) {
-        const uint32_t g = g0 + threadIdx.x / lanes;
-        double t1 = 0.0, t2 = 0.0;
-        if (g < a.groups) {
-            const double *at = part + ((uint64_t)n * a.groups + g) * p.chunks * 2;
+    const double *at = part + sample_and_group * p.chunks * 2;
+    double t1 = 0.0, t2 = 0.0;
 #pragma unroll 4
-            for (uint32_t c = lane; c < p.chunks; c += lanes) { t1 += at[2 * c]; t2 += at[2 * c + 1]; }
-        }
-        for (uint32_t k = lanes >> 1; k > 0; k >>= 1) { t1 += __shfl_xor(t1, k); t2 += __shfl_xor(t2, k); }
-        if (g < a.groups && lane == 0) { s[2 * g] = t1; s[2 * g + 1] = t2; }
+    for (uint32_t c = threadIdx.x & 63u; c < p.chunks; c += 64u) { t1 += at[2 * c]; t2 += at[2 * c + 1]; }
+    return {wave_sum(t1), wave_sum(t2)};
+}
+
+// Mean and 1 / deviation of every sample and group, between the two passes.  A launch of its own costs 3 us; with this in
+// the prologue of the second pass's workgroups, each of them reads all of its sample's partial sums (one sample of
+// 65536 x 128: 41.6 us where the three launches take 33.8; 64 samples of 3136 x 256: 72 and 76).
+__global__ __launch_bounds__(kMaxThreads) void k_norm_join(NormArgs a, Plan p, double *stats)
+{
+    const uint64_t i = (uint64_t)blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6);
+    if (i >= a.batch * a.groups) return;
+    const Totals t = join_chunks(static_cast<const double *>(a.work), i, p);
+    const Moments v = moments_of(a, p, t.t1, t.t2);
+    if ((threadIdx.x & 63u) == 0) {
+        stats[2 * i] = v.mean;
+        stats[2 * i + 1] = v.rstd;
     }
-    __syncthreads();
 }
 
 template <uint32_t T, uint32_t F, bool EVEN>
-__global__ __launch_bounds__(kMaxThreads) void k_norm_apply(NormArgs a, Plan p)
+__global__ __launch_bounds__(kMaxThreads) void k_norm_apply(NormArgs a, Plan p, const double *stats)
 {
-    extern __shared__ double s_sum[];
     typedef typename ElemOf<T>::type E;
     const Place q = place(p, blockIdx.x, 0, a.channels);
     const uint32_t beg = q.chunk * p.rows_per, end = a.spatial - beg < p.rows_per ? a.spatial : beg + p.rows_per;
@@ -401,18 +416,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_apply(NormArgs a, Plan p)
         return load_vector<T, EVEN>(src + (n > 0 ? (row0 + r) * a.channels : 0), n);
     };
     Line l = parameters_of(a, q);
-    join_chunks(s_sum, static_cast<const double *>(a.work), q.n, a, p);
-    for (uint32_t g = threadIdx.x; g < a.groups; g += blockDim.x) {
-        const Moments v = moments_of(a, p, s_sum[2 * g], s_sum[2 * g + 1]);
-        s_sum[2 * g] = v.mean;
-        s_sum[2 * g + 1] = v.rstd;
-        if (q.chunk == 0 && a.stats) {
-            a.stats[((uint64_t)q.n * a.groups + g) * 2] = v.mean;
-            a.stats[((uint64_t)q.n * a.groups + g) * 2 + 1] = v.rstd;
-        }
-    }
-    __syncthreads();
-    apply_moments(&l, p, q, s_sum, 0);
+    apply_moments(&l, p, q, stats + 2ull * q.n * a.groups, 0);
     if (F != kPlain) put_tail(a);
     // every thread of the workgroup goes round as often: the lanes of a quantisation group meet in put_outputs
     f32x8 next = fetch(beg);
@@ -768,22 +772,33 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_sums(NormArgs a, Plan
     }
 }
 
-template <uint32_t T, uint32_t S, uint32_t ACT, bool ONE>
-__global__ __launch_bounds__(kMaxThreads) void k_norm_grad_apply(NormArgs a, Plan p, uint32_t param_blocks)
+// Between the two passes: the totals A and B of every sample and group, and the parameters' gradients.
+__global__ __launch_bounds__(kMaxThreads) void k_norm_grad_join(NormArgs a, Plan p, double *totals, uint32_t param_blocks)
 {
     extern __shared__ double s_sum[];
-    typedef typename ElemOf<T>::type E;
     const double *part = static_cast<const double *>(a.work);
     if (blockIdx.x < param_blocks) {
         join_parameters(s_sum, a, reinterpret_cast<const float *>(part + 2ull * a.batch * a.groups * p.chunks),
                         a.spatial ? a.batch * p.chunks : 0, blockIdx.x);
         return;
     }
-    const Place q = place(p, blockIdx.x - param_blocks, 0, a.channels);
-    join_chunks(s_sum, part, q.n, a, p);
+    const uint64_t i = (uint64_t)(blockIdx.x - param_blocks) * (blockDim.x >> 6) + (threadIdx.x >> 6);
+    if (i >= a.batch * a.groups) return;
+    const Totals t = join_chunks(part, i, p);
+    if ((threadIdx.x & 63u) == 0) {
+        totals[2 * i] = t.t1;
+        totals[2 * i + 1] = t.t2;
+    }
+}
+
+template <uint32_t T, uint32_t S, uint32_t ACT, bool ONE>
+__global__ __launch_bounds__(kMaxThreads) void k_norm_grad_apply(NormArgs a, Plan p, const double *totals)
+{
+    typedef typename ElemOf<T>::type E;
+    const Place q = place(p, blockIdx.x, 0, a.channels);
     const Channels<ONE> ch = channels_of<ONE>(a, p, q);
     float ga[ONE ? 1 : 8], gb[ONE ? 1 : 8];
-    pick_totals<ONE>(s_sum, a, p, q, 0, ga, gb);
+    pick_totals<ONE>(totals + 2ull * q.n * a.groups, a, p, q, 0, ga, gb);
     each_gradient<T, S, ACT, ONE>(a, p, q, ch, [&](uint64_t row, f32x8 du, f32x8 h) {
         store8<T>(static_cast<E *>(a.y) + row * a.channels + q.c, input_gradient<ONE>(ch, du, h, ga, gb), q.valid);
     });
@@ -797,7 +812,14 @@ size_t lds_bytes(const Plan &p, size_t per_thread, size_t groups, bool both)
     const size_t joined = p.threads * per_thread, totals = 16 * groups;
     return both ? joined + totals : joined > totals ? joined : totals;
 }
-size_t moment_bytes(const Plan &p) { return p.per & 7u ? 128 : 16; }
+uint32_t join_blocks(const NormArgs &a) { return (uint32_t)((a.batch * a.groups + kMaxThreads / 64 - 1) / (kMaxThreads / 64)); }
+// What the first pass leaves in the workspace: two totals per sample, range and group; backward: two sums per channel behind them.
+uint64_t records_bytes(const NormArgs &a, const Plan &p, bool backward)
+{
+    const uint64_t records = a.batch * p.chunks;
+    return (records * (16ull * a.groups + (backward ? 8ull * a.channels : 0ull)) + 15) & ~15ull;
+}
+size_t moment_bytes(const Plan &p) { return p.per < 8u ? 128 : 32; }
 
 template <uint32_t T, uint32_t F, bool EVEN>
 void forward_as(const NormArgs &a, hipStream_t st)
@@ -812,7 +834,9 @@ void forward_as(const NormArgs &a, hipStream_t st)
     p = two_pass_plan(a, lanes);
     const dim3 grid((uint32_t)(a.batch * p.chunks)), block(p.threads);
     hipLaunchKernelGGL((k_norm_sums<T, EVEN>), grid, block, lds_bytes(p, moment_bytes(p), 0, false), st, a, p);
-    hipLaunchKernelGGL((k_norm_apply<T, F, EVEN>), grid, block, lds_bytes(p, 0, a.groups, false), st, a, p);
+    double *stats = a.stats ? a.stats : static_cast<double *>(a.work) + 2ull * a.batch * a.groups * p.chunks;
+    hipLaunchKernelGGL(k_norm_join, dim3(join_blocks(a)), dim3(kMaxThreads), 0, st, a, p, stats);
+    hipLaunchKernelGGL((k_norm_apply<T, F, EVEN>), grid, block, 0, st, a, p, stats);
 }
 
 template <uint32_t T, uint32_t S, uint32_t ACT, bool ONE>
@@ -828,11 +852,13 @@ void backward_as(const NormArgs &a, hipStream_t st)
     }
     p = two_pass_plan(a, 1);
     const uint32_t work = a.spatial ? (uint32_t)(a.batch * p.chunks) : 0;
+    double *totals = reinterpret_cast<double *>(static_cast<uint8_t *>(a.work) + records_bytes(a, p, true));
+    const uint32_t joins = work ? join_blocks(a) : 0;
     if (work)
         hipLaunchKernelGGL((k_norm_grad_sums<T, S, ACT, ONE>), dim3(work), dim3(p.threads), lds_bytes(p, 64, 0, false) + 32 * p.nv, st, a, p);
-    if (work + params)
-        hipLaunchKernelGGL((k_norm_grad_apply<T, S, ACT, ONE>), dim3(work + params), dim3(p.threads), lds_bytes(p, 8, a.groups, false),
-                           st, a, p, params);
+    if (params + joins)
+        hipLaunchKernelGGL(k_norm_grad_join, dim3(params + joins), dim3(kMaxThreads), 8 * kMaxThreads, st, a, p, totals, params);
+    if (work) hipLaunchKernelGGL((k_norm_grad_apply<T, S, ACT, ONE>), dim3(work), dim3(p.threads), 0, st, a, p, totals);
 }
 
 template <uint32_t T, uint32_t S, uint32_t ACT>
@@ -881,8 +907,7 @@ uint64_t group_norm_work(const NormArgs &a)
 {
     uint64_t most = 8ull * a.batch * a.channels;                          // sums of every sample, per channel
     for (uint32_t lanes : {1u, 4u, 8u, 16u}) {
-        const uint64_t records = a.batch * two_pass_plan(a, lanes).chunks;
-        const uint64_t bytes = records * (16ull * a.groups + (lanes == 1u ? 8ull * a.channels : 0ull));
+        const uint64_t bytes = records_bytes(a, two_pass_plan(a, lanes), lanes == 1u) + 16ull * a.batch * a.groups;
         if (bytes > most) most = bytes;
     }
     return most;
