@@ -361,7 +361,7 @@ int cmp_byte_linear_grad(int device, const cmp_byte_shape *shape, const void *d_
  * d_gamma, d_beta: fp32, one per channel, either may be NULL (ones, zeros).  d_stats (double, [batch][groups][2]: mean,
  * 1 / sqrt(var + eps)) is written for the backward pass; NULL: not wanted.  With d_ck the input is kept as a byte
  * checkpoint of batch * spatial rows in the same pass, the bytes of cmp_byte_store; NULL: not kept.
- * d_work: cmp_group_norm_work bytes, aligned to 16, used during a call only, the same for both directions.
+ * d_work: cmp_group_norm_work bytes (it may be 0), aligned to 16, used during a call only, the same for both directions.
  * cmp_group_norm_grad takes the input d_x OR its checkpoint d_ck (the other NULL), gamma, beta and d_stats of
  * the forward pass, and gives, with u = h * gamma + beta from the restored input and du = dy * act'(u),
  *    dbeta = sum du,  dgamma = sum du * h   (fp32, overwritten; either may be NULL)

@@ -202,8 +202,9 @@ int cmp_group_norm(int device, const cmp_norm_shape *shape, const void *d_x, con
     if (!empty && (!d_x || !d_y || misaligned(d_x, es) || misaligned(d_y, es))) return CMP_E_ARG;
     if (misaligned(d_gamma, 4) || misaligned(d_beta, 4) || misaligned(d_stats, 8)) return CMP_E_ARG;
     if (d_ck && (rc = norm_checkpoint(&a, *shape, format, group, d_ck, cap, CMP_E_NOSPACE)) != CMP_OK) return rc;
-    if (!empty && work_bytes < group_norm_work(a)) return CMP_E_NOSPACE;
-    if (!empty && (!d_work || misaligned(d_work, 16))) return CMP_E_ARG;
+    const uint64_t need = empty ? 0 : group_norm_work(a);
+    if (work_bytes < need) return CMP_E_NOSPACE;
+    if (need && (!d_work || misaligned(d_work, 16))) return CMP_E_ARG;
     DeviceGuard guard(device);
     if (guard.rc != CMP_OK) return guard.rc;
     if (empty) return CMP_OK;
@@ -232,8 +233,9 @@ int cmp_group_norm_grad(int device, const cmp_norm_shape *shape, const void *d_d
         misaligned(d_dbeta, 4))
         return CMP_E_ARG;
     if (d_ck && (rc = norm_checkpoint(&a, *shape, format, group, d_ck, bytes, CMP_E_FORMAT)) != CMP_OK) return rc;
-    if (!empty && work_bytes < group_norm_work(a)) return CMP_E_NOSPACE;
-    if (!empty && (!d_work || misaligned(d_work, 16))) return CMP_E_ARG;
+    const uint64_t need = empty ? 0 : group_norm_work(a);
+    if (work_bytes < need) return CMP_E_NOSPACE;
+    if (need && (!d_work || misaligned(d_work, 16))) return CMP_E_ARG;
     DeviceGuard guard(device);
     if (guard.rc != CMP_OK) return guard.rc;
     a.x = d_x;

@@ -392,13 +392,13 @@ __device__ __forceinline__ Totals join_chunks(const double *part, uint64_t sampl
 // 65536 x 128: 41.6 us where the three launches take 33.8; 64 samples of 3136 x 256: 72 and 76).
 __global__ __launch_bounds__(kMaxThreads) void k_norm_join(NormArgs a, Plan p, double *stats)
 {
-    const uint64_t i = (uint64_t)blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6);
-    if (i >= a.batch * a.groups) return;
-    const Totals t = join_chunks(static_cast<const double *>(a.work), i, p);
-    const Moments v = moments_of(a, p, t.t1, t.t2);
-    if ((threadIdx.x & 63u) == 0) {
-        stats[2 * i] = v.mean;
-        stats[2 * i + 1] = v.rstd;
+    for (uint64_t i = blockIdx.x * 16ull + (threadIdx.x >> 6); i < a.batch * a.groups; i += gridDim.x * 16ull) {
+        const Totals t = join_chunks(static_cast<const double *>(a.work), i, p);
+        const Moments v = moments_of(a, p, t.t1, t.t2);
+        if ((threadIdx.x & 63u) == 0) {
+            stats[2 * i] = v.mean;
+            stats[2 * i + 1] = v.rstd;
+        }
     }
 }
 
@@ -782,12 +782,13 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_join(NormArgs a, Plan
                         a.spatial ? a.batch * p.chunks : 0, blockIdx.x);
         return;
     }
-    const uint64_t i = (uint64_t)(blockIdx.x - param_blocks) * (blockDim.x >> 6) + (threadIdx.x >> 6);
-    if (i >= a.batch * a.groups) return;
-    const Totals t = join_chunks(part, i, p);
-    if ((threadIdx.x & 63u) == 0) {
-        totals[2 * i] = t.t1;
-        totals[2 * i + 1] = t.t2;
+    const uint64_t step = (gridDim.x - param_blocks) * 16ull;
+    for (uint64_t i = (blockIdx.x - param_blocks) * 16ull + (threadIdx.x >> 6); i < a.batch * a.groups; i += step) {
+        const Totals t = join_chunks(part, i, p);
+        if ((threadIdx.x & 63u) == 0) {
+            totals[2 * i] = t.t1;
+            totals[2 * i + 1] = t.t2;
+        }
     }
 }
 
@@ -812,7 +813,11 @@ size_t lds_bytes(const Plan &p, size_t per_thread, size_t groups, bool both)
     const size_t joined = p.threads * per_thread, totals = 16 * groups;
     return both ? joined + totals : joined > totals ? joined : totals;
 }
-uint32_t join_blocks(const NormArgs &a) { return (uint32_t)((a.batch * a.groups + kMaxThreads / 64 - 1) / (kMaxThreads / 64)); }
+uint32_t join_blocks(const NormArgs &a)                                   // sixteen waves, a sample and group each
+{
+    const uint64_t n = (a.batch * a.groups + kMaxThreads / 64 - 1) / (kMaxThreads / 64);
+    return (uint32_t)(n < 65536 ? n : 65536);
+}
 // What the first pass leaves in the workspace: two totals per sample, range and group; backward: two sums per channel behind them.
 uint64_t records_bytes(const NormArgs &a, const Plan &p, bool backward)
 {
@@ -905,9 +910,12 @@ void forward_of(const NormArgs &a, hipStream_t st)
 // position takes).
 uint64_t group_norm_work(const NormArgs &a)
 {
-    uint64_t most = 8ull * a.batch * a.channels;                          // sums of every sample, per channel
+    uint64_t most = 0;
     for (uint32_t lanes : {1u, 4u, 8u, 16u}) {
-        const uint64_t bytes = records_bytes(a, two_pass_plan(a, lanes), lanes == 1u) + 16ull * a.batch * a.groups;
+        Plan p;
+        uint64_t bytes;
+        if (slab_plan(&p, a, lanes)) bytes = lanes == 1u && a.batch > 1 ? 8ull * a.batch * a.channels : 0;    // sums of every sample
+        else bytes = records_bytes(a, two_pass_plan(a, lanes), lanes == 1u) + 16ull * a.batch * a.groups;
         if (bytes > most) most = bytes;
     }
     return most;

@@ -580,6 +580,7 @@ Choice choose(uint64_t rows, uint64_t cols, uint64_t outs, uint32_t type)
         double best = 0;
         for (int i = 0; i < kTileCount; ++i) {
             const uint64_t tiles = ((outs + kTiles[i].n - 1) / kTiles[i].n) * ((cols + kTiles[i].k - 1) / kTiles[i].k);
+            if (tiles > (1u << 22)) continue;                             // threads of a launch are counted with 32 bits
             // one range, and as many as fill a quarter of the CUs, half of them, all of them once, twice, ...
             for (uint64_t fill : {0ull, 64ull, 128ull, 256ull, 512ull, 768ull, 1024ull}) {
                 uint64_t k = fill / tiles;

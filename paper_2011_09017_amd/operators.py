@@ -170,6 +170,7 @@ def byte_linear_grad(dy: torch.Tensor, ck: ByteCheckpoint, bias: bool = False, d
     outs, cols = int(dy.shape[-1]), ck.cols
     _refuse(accumulate and out is None, "byte_linear_grad: accumulate needs out")
     _refuse(accumulate and bias and out_bias is None, "byte_linear_grad: accumulate with a bias needs out_bias")
+    _refuse(out is not None and dtype is not None and out.dtype != dtype, "byte_linear_grad: out has another type than dtype")
     dtype = out.dtype if out is not None else dtype or dy.dtype
     _refuse(dtype not in (dy.dtype, torch.float32), "byte_linear_grad: results are in dy's type or float32")
     if out is None:
@@ -224,10 +225,10 @@ def group_norm(x: torch.Tensor, groups: int, weight: Optional[torch.Tensor] = No
         held, nbytes = _byte_shape(shape.batch * shape.spatial, shape.channels, save, group)
         fmt = held.format
         ck = ByteCheckpoint(torch.empty(nbytes, dtype=torch.uint8, device=dev), tuple(x.shape), x.dtype, save, group)
-    work = torch.empty(need, dtype=torch.uint8, device=dev)
+    work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     _call(binding.cmp_group_norm(dev.index, shape, x.data_ptr(), gamma, beta, y.data_ptr(), stats.data_ptr(), fmt, group,
-                                 None if ck is None else ck.buf.data_ptr(), 0 if ck is None else ck.buf.numel(), work.data_ptr(),
-                                 need, _stream(dev)), "cmp_group_norm")
+                                 None if ck is None else ck.buf.data_ptr(), 0 if ck is None else ck.buf.numel(),
+                                 None if work is None else work.data_ptr(), need, _stream(dev)), "cmp_group_norm")
     return y, stats, ck
 
 
@@ -251,9 +252,9 @@ def group_norm_grad(dy: torch.Tensor, x, stats: torch.Tensor, groups: int, weigh
     dweight = dbias = None
     if params:
         dweight, dbias = torch.empty(2, dy.shape[-1], dtype=torch.float32, device=dev).unbind(0)
-    work = torch.empty(need, dtype=torch.uint8, device=dev)
+    work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     _call(binding.cmp_group_norm_grad(dev.index, shape, dy.data_ptr(), None if held else x.data_ptr(), fmt, group,
                                       src.data_ptr() if held else None, src.numel() if held else 0, gamma, beta, stats.data_ptr(),
                                       dx.data_ptr(), dweight.data_ptr() if params else None, dbias.data_ptr() if params else None,
-                                      work.data_ptr(), need, _stream(dev)), "cmp_group_norm_grad")
+                                      None if work is None else work.data_ptr(), need, _stream(dev)), "cmp_group_norm_grad")
     return dx, dweight, dbias

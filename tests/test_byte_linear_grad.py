@@ -84,6 +84,31 @@ def test_gradients(rows, cols, outs, dtype, fmt, group):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols,outs", [(4099, 2047, 1531), (1000, 520, 776), (2500, 64, 2056), (3000, 1100, 70), (1537, 1025, 263),
+                                            (300, 4000, 3), (2000, 9, 520)])
+@pytest.mark.parametrize("dtype", list(TERMS))
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_larger_products(rows, cols, outs, dtype, fmt):
+    """Every size of tile, several ranges of rows, edges that nothing divides, a NaN in one column; float64 on the GPU."""
+    ck, dy = _case(rows, cols, outs, dtype, fmt, 64)
+    nan_at = (rows - 1) * ((cols + 15) // 16 * 16) + cols // 2
+    ck.buf[nan_at] = 0x80 if fmt == "int8" else 0x7f
+    x = ops.byte_load(ck, dtype=torch.float32).double()
+    assert int(torch.isnan(x).sum()) == 1
+    fine = torch.arange(cols, device="cuda") != cols // 2
+    x = torch.nan_to_num(x)
+    y = dy.double()
+    want, size = torch.mm(y.t().contiguous(), x), torch.mm(y.abs().t().contiguous(), x.abs())
+    start = torch.randn(outs, cols, generator=torch.Generator().manual_seed(1)).cuda()
+    dw, db = ops.byte_linear_grad(dy, ck, bias=True)
+    assert bool(torch.isnan(dw[:, ~fine]).all()) and bool(torch.isfinite(dw[:, fine]).all())
+    _close(dw[:, fine], want[:, fine].cpu(), size[:, fine].cpu(), rows * TERMS[dtype])
+    _close(db, y.sum(0).cpu(), y.abs().sum(0).cpu(), rows * TERMS[dtype])
+    sums, _ = ops.byte_linear_grad(dy, ck, out=start.clone(), accumulate=True)
+    _close(sums[:, fine], (want + start.double())[:, fine].cpu(), (size + start.abs().double())[:, fine].cpu(), rows * TERMS[dtype] + 1)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", list(TERMS))
 @pytest.mark.parametrize("rows,cols,outs", [(40, 70, 33), (9000, 64, 48)])
 def test_accumulates(dtype, rows, cols, outs):
@@ -175,6 +200,7 @@ def test_refusals_on_the_gpu():
                  lambda: ops.byte_linear_grad(dy, ck, accumulate=True), lambda: ops.byte_linear_grad(dy, ck, out=f.t()),
                  lambda: ops.byte_linear_grad(dy, ck, out=f[:, :39]), lambda: ops.byte_linear_grad(dy, ck, out=f, bias=True, accumulate=True),
                  lambda: ops.byte_linear_grad(dy, ck, out=f, out_bias=torch.zeros(24, device="cuda").bfloat16()),
-                 lambda: ops.byte_linear_grad(dy.cpu(), ck), lambda: ops.byte_linear_grad(dy.double(), ck)):
+                 lambda: ops.byte_linear_grad(dy.cpu(), ck), lambda: ops.byte_linear_grad(dy.double(), ck),
+                 lambda: ops.byte_linear_grad(dy, ck, out=f, dtype=torch.bfloat16)):
         with pytest.raises(ValueError):
             call()

@@ -38,6 +38,7 @@ def test_library_refusals():
         s = b.cmp_norm_shape(**{**good, **bad})
         assert b.cmp_group_norm_work(s) == 0, bad
         assert both(s) == (b.CMP_E_ARG, b.CMP_E_ARG), bad
+    assert b.cmp_group_norm_work(b.cmp_norm_shape(**{**good, 'batch': 1})) == 0      # one pass, nothing between workgroups
     s = b.cmp_norm_shape(**good)
     need = b.cmp_group_norm_work(s)
     for kw in (dict(x=0), dict(x=P + 2), dict(y=0), dict(y=P + 1), dict(gamma=P + 2), dict(stats=P + 4), dict(work=P + 8), dict(work=0),
@@ -130,7 +131,9 @@ def _check_backward(dy, xd, stats, groups, w, b, act, dx, dw, db):
 
 
 SHAPES = [(1, 1, 1, 1), (1, 1, 8, 8), (2, 49, 512, 32), (3, 7, 30, 3), (1, 1000, 10, 1), (2, 3025, 96, 8), (5, 1, 64, 4), (1, 5, 8192, 4096),
-          (2, 33, 8192, 1), (7, 13, 40, 4), (300, 4, 24, 2), (1, 4097, 320, 32), (2, 196, 1000, 125), (1, 2, 4100, 2)]
+          (2, 33, 8192, 1), (7, 13, 40, 4), (300, 4, 24, 2), (1, 4097, 320, 32), (2, 196, 1000, 125), (1, 2, 4100, 2),
+          # two passes: groups narrower than a vector with the widest rows, rows of more than 512 vectors, and one group of all
+          (1, 600, 8192, 4096), (2, 530, 4104, 171), (3, 1500, 30, 10), (1, 9000, 64, 1), (40, 600, 128, 16)]
 
 
 @pytest.mark.gpu
