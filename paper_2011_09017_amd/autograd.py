@@ -18,6 +18,7 @@ eight bits per value instead: :class:`ByteCheckpoints` are hooks of the same kin
 """
 from __future__ import annotations
 
+import math
 import weakref
 from dataclasses import dataclass
 from typing import Callable, Iterable, Optional, Union
@@ -187,7 +188,8 @@ class ByteCheckpoints:
     dense).  A graph can be walked backward as often as autograd allows: checkpoints are only read.
 
     fmt, group: see operators.byte_store.  min_numel: smaller tensors are saved as they are, and so are parameters,
-    tensors named to skip_parameters and tensors with gaps.  A value is off by at most 1/127 of the largest in its group
+    tensors named to skip_parameters, tensors with gaps and those whose rows are too short for eight bits to save anything (a
+    row of codes takes a multiple of 16 bytes).  A value is off by at most 1/127 of the largest in its group
     ("int8") or 1/16 of itself ("e4m3"): what is not an activation (indices kept as floats, running sums) does not
     belong under these hooks.
     """
@@ -202,10 +204,16 @@ class ByteCheckpoints:
         for p in params:
             self._skip.add(p.data_ptr())
 
+    def _held_bytes(self, t: torch.Tensor, order: tuple) -> int:
+        cols = t.shape[order[-1]]
+        return operators._byte_shape(t.numel() // cols, cols, self.fmt, self.group)[1]
+
     def pack(self, t: torch.Tensor):
-        order = tuple(sorted(range(t.dim()), key=lambda d: (-t.stride(d), d)))
+        # dimensions of one element last in the order of memory would make rows of one value: they come first
+        order = tuple(sorted(range(t.dim()), key=lambda d: (t.shape[d] != 1, -t.stride(d), d)))
         if (not t.is_cuda or t.dtype not in operators._TYPES or t.dim() < 1 or t.numel() < max(1, self.min_numel)
-                or isinstance(t, torch.nn.Parameter) or t.data_ptr() in self._skip or not t.permute(order).is_contiguous()):
+                or isinstance(t, torch.nn.Parameter) or t.data_ptr() in self._skip or not t.permute(order).is_contiguous()
+                or self._held_bytes(t, order) >= t.numel() * t.element_size()):
             self.stats["passed_through"] += 1
             return t
         ck = operators.byte_store(t.detach().permute(order), self.fmt, self.group)
@@ -232,30 +240,52 @@ def _dense_rows(t: torch.Tensor) -> torch.Tensor:
     return t if operators._rows_of(t) is not None else t.contiguous()
 
 
+def _as_matrix(t: torch.Tensor) -> torch.Tensor:
+    return t.reshape(math.prod(t.shape[:-1]), t.shape[-1])
+
+
+def _keep(ctx, held: Optional[operators.ByteCheckpoint], *tensors) -> None:
+    """Saves tensors and a checkpoint for the backward pass; autograd frees its bytes with the others behind that pass."""
+    ctx.held = None if held is None else held._replace(buf=None)
+    ctx.save_for_backward(*tensors, None if held is None else held.buf)
+
+
+def _kept(ctx):
+    *tensors, buf = ctx.saved_tensors
+    return None if buf is None else ctx.held._replace(buf=buf), *tensors
+
+
+def _product(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor]) -> torch.Tensor:
+    """The linear layer of a matrix: with more dimensions torch may choose a batched product."""
+    return torch.nn.functional.linear(_as_matrix(x), weight, bias).view(*x.shape[:-1], weight.shape[0])
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
     @torch.amp.custom_fwd(device_type="cuda")
     def forward(ctx, x, weight, bias, fmt, group):
-        ctx.held = operators.byte_store(_dense_rows(x), fmt, group) if ctx.needs_input_grad[1] else None
-        ctx.save_for_backward(weight if ctx.needs_input_grad[0] else None)
+        rows = _dense_rows(x)
+        held = operators.byte_store(rows, fmt, group) if ctx.needs_input_grad[1] else None
+        _keep(ctx, held, weight if ctx.needs_input_grad[0] else None)
         ctx.kinds = (x.dtype, weight.dtype, None if bias is None else bias.dtype)
-        return torch.nn.functional.linear(x, weight, bias)
+        return _product(rows, weight, bias)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     @torch.amp.custom_bwd(device_type="cuda")
     def backward(ctx, dy):
-        (weight,) = ctx.saved_tensors
+        held, weight = _kept(ctx)
         dx = dw = db = None
+        dy = _dense_rows(dy)
         if ctx.needs_input_grad[0]:
-            dx = torch.matmul(dy, weight.to(dy.dtype)).to(ctx.kinds[0])
+            dx = torch.mm(_as_matrix(dy), weight.to(dy.dtype)).to(ctx.kinds[0]).view(*dy.shape[:-1], weight.shape[1])
         with_bias = ctx.kinds[2] is not None and ctx.needs_input_grad[2]
         if ctx.needs_input_grad[1]:
             dtype = torch.float32 if ctx.kinds[1] == torch.float32 else dy.dtype
-            dw, db = operators.byte_linear_grad(_dense_rows(dy), ctx.held, bias=with_bias, dtype=dtype)
+            dw, db = operators.byte_linear_grad(dy, held, bias=with_bias, dtype=dtype)
             dw = dw.to(ctx.kinds[1])
         elif with_bias:
-            db = dy.reshape(-1, dy.shape[-1]).sum(0, dtype=torch.float32)
+            db = _as_matrix(dy).sum(0, dtype=torch.float32)
         if db is not None:
             db = db.to(ctx.kinds[2])
         return dx, dw, db, None, None
@@ -263,7 +293,11 @@ class _Linear(torch.autograd.Function):
 
 def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, fmt: str = "int8", group: int = 64):
     """torch.nn.functional.linear whose input is held as a byte checkpoint; the weight's (and bias's) gradient is computed from
-    the eight-bit form by operators.byte_linear_grad.  x: [..., cols] in float32, float16 or bfloat16 on a GPU."""
+    the eight-bit form by operators.byte_linear_grad.  x: [..., cols] in float32, float16 or bfloat16 on a GPU.  Without a
+    backward pass to come (torch.no_grad) nothing is stored."""
+    operators._byte_shape(0, 0, fmt, group)                           # refuses a bad format in either case
+    if not torch.is_grad_enabled():
+        return _product(x, weight, bias)
     return _Linear.apply(x, weight, bias, fmt, group)
 
 
@@ -273,17 +307,17 @@ class _GroupNorm(torch.autograd.Function):
         x = x.contiguous()
         w, b = (None if p is None else p.float().contiguous() for p in (weight, bias))
         y, stats, held = operators.group_norm(x, groups, w, b, eps, act, save=fmt, group=group)
-        ctx.held, ctx.groups, ctx.act = held, groups, act
+        ctx.groups, ctx.act = groups, act
         ctx.kinds = tuple(None if p is None else p.dtype for p in (weight, bias))
-        ctx.save_for_backward(w, b, stats, None if held is not None else x)
+        _keep(ctx, held, w, b, stats, None if held is not None else x)
         return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        w, b, stats, x = ctx.saved_tensors
+        held, w, b, stats, x = _kept(ctx)
         params = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
-        dx, dw, db = operators.group_norm_grad(dy.contiguous(), ctx.held if x is None else x, stats, ctx.groups, w, b, ctx.act,
+        dx, dw, db = operators.group_norm_grad(dy.contiguous(), held if x is None else x, stats, ctx.groups, w, b, ctx.act,
                                                params=params)
         dw = dw.to(ctx.kinds[0]) if params and ctx.needs_input_grad[1] else None
         db = db.to(ctx.kinds[1]) if params and ctx.needs_input_grad[2] else None
@@ -294,5 +328,7 @@ def group_norm(x: torch.Tensor, groups: int, weight: Optional[torch.Tensor] = No
                eps: float = 1e-5, act: str = "none", fmt: Optional[str] = "int8", group: int = 64):
     """Group norm and activation of x[batch, ..., channels] (channels last: permute an NCHW tensor to NHWC first, which costs
     nothing for one in torch's channels_last format).  Its input is held as a byte checkpoint written in the same pass;
-    fmt=None holds x itself."""
-    return _GroupNorm.apply(x, weight, bias, groups, eps, act, fmt, group)
+    fmt=None holds x itself.  Without a backward pass to come (torch.no_grad) nothing is stored."""
+    if fmt is not None:
+        operators._byte_shape(0, 0, fmt, group)                       # refuses a bad format in either case
+    return _GroupNorm.apply(x, weight, bias, groups, eps, act, fmt if torch.is_grad_enabled() else None, group)

@@ -22,6 +22,82 @@ def test_hooks_refuse_and_pass_through_without_a_gpu():
     assert held.stats["packed"] == 0 and torch.equal(x.grad, 2 * x.detach())
 
 
+def test_without_gradients_nothing_is_stored_and_formats_are_checked():
+    x, w = torch.randn(3, 5, 32), torch.randn(7, 32, requires_grad=True)
+    with torch.no_grad():
+        assert torch.equal(linear(x, w), torch.nn.functional.linear(x, w))       # no GPU is needed where nothing is stored
+        for layer in (lambda **kw: linear(x, w, **kw), lambda **kw: group_norm(x, 4, **kw)):
+            for kw in (dict(fmt="int4"), dict(group=48)):
+                with pytest.raises(ValueError):
+                    layer(**kw)
+
+
+@pytest.mark.gpu
+def test_norm_without_gradients_stores_nothing(monkeypatch):
+    asked = []
+    real = ops.group_norm
+    monkeypatch.setattr(ops, "group_norm", lambda *a, **kw: (asked.append(kw["save"]), real(*a, **kw))[1])
+    x = torch.randn(2, 9, 32, device=DEV, requires_grad=True)
+    with torch.no_grad():
+        y = group_norm(x, 4)
+    assert torch.equal(y, group_norm(x, 4).detach()) and asked == [None, "int8"]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("what", ["linear", "norm"])
+def test_checkpoints_go_with_the_backward_pass(what):
+    """Once the backward pass is over its checkpoints are free, also while the loss is held, and a second pass is refused."""
+    x = torch.randn(4, 1024, 512, device=DEV).bfloat16()
+    w = torch.randn(512, 512, device=DEV).bfloat16().requires_grad_() if what == "linear" else torch.ones(512, device=DEV, requires_grad=True)
+    w.grad = torch.zeros_like(w)
+    layer = (lambda: linear(x, w)) if what == "linear" else (lambda: group_norm(x, 8, w))
+    layer().sum().backward()                                     # the workspaces that torch's library calls keep for good
+    before = torch.cuda.memory_allocated()
+    loss = layer().sum()
+    held = 4 * 1024 * (512 + 512 // 64)
+    assert torch.cuda.memory_allocated() >= before + held
+    loss.backward()
+    torch.cuda.synchronize()
+    assert torch.cuda.memory_allocated() < before + held
+    with pytest.raises(RuntimeError):
+        loss.backward()
+
+
+@pytest.mark.gpu
+def test_linear_of_uneven_rows_and_of_nothing():
+    """Inputs and gradients whose rows are not evenly spaced, gradients that are one expanded value, and no rows at all.  Two bf16
+    roundings of sums in another order: 2 * 2^-8 of the value; fp32 sums of 48 terms below 16: 48 * 48 * 16 * 2^-24 = 2.2e-3 at the
+    very most, of which signs leave far less: 1e-3."""
+    near = dict(rtol=2 ** -7, atol=1e-3)
+    x, w, b = _layer(torch.bfloat16, 60, 48, 40)
+    base = x.detach().view(3, 20, 48)
+    for x3 in (base.transpose(0, 1), base[:, :1].expand(3, 20, 48), base[:, ::2], base[:, :0], base[0, 0]):
+        x3 = x3.detach().requires_grad_()
+        for bias in (b, None):
+            y = linear(x3, w, bias)
+            assert torch.allclose(y, torch.nn.functional.linear(x3.detach().contiguous().view(-1, 48), w, bias).view(y.shape), **near)
+            dy = torch.ones(1, dtype=y.dtype, device=DEV).expand(y.shape)
+            dx, dw = torch.autograd.grad(y, (x3, w), dy)
+            assert torch.allclose(dx, torch.mm(dy.reshape(-1, 40), w.detach()).view(x3.shape), **near)
+            assert torch.equal(dw, ops.byte_linear_grad(dy.contiguous(), ops.byte_store(x3.detach().contiguous()))[0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,packs", [((5000, 1), True), ((3000, 3), False), ((64, 32, 1, 1), True), ((1, 4096), True),
+                                         ((1000, 2, 8), False), ((1000, 9), True), ((1000, 16), True)])
+def test_hooks_hold_only_what_gets_smaller(shape, packs):
+    """bf16, groups of 32: a row takes 16 bytes of codes and one of its exponent at least, which is more than 3 or 8 values take as
+    they are and less than 9 (a last dimension of one element counts as none)."""
+    held = ByteCheckpoints("int8", 32, min_numel=1)
+    x = torch.randn(shape, device=DEV).bfloat16()
+    h = held.pack(x)
+    assert (h is not x) == packs
+    if packs:
+        assert h.ck.nbytes < 2 * x.numel() and held.unpack(h).shape == x.shape
+        flat = [n for n in shape if n != 1]
+        assert torch.equal(held.unpack(h).view(flat), ops.byte_load(ops.byte_store(x.view(flat), "int8", 32)))
+
+
 def _layer(dtype, rows, cols, outs, seed=0):
     gen = torch.Generator().manual_seed(seed)
     x = torch.randn(rows, cols, generator=gen).to(dtype).to(DEV)
