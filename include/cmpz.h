@@ -311,8 +311,8 @@ int cmp_estimate_eb(cmp_ctx *ctx, const float *d_act, uint64_t act_numel, const 
  *                    even to e4m3 (4 exponent bits, bias 7, 3 mantissa bits, largest 448, 0x7f and 0xff NaN); NaN for
  *                    NaN and infinities;
  *    x' = code * 2^e in both.
- * So |x - x'| <= 2^(e-1) (CMP_BYTE_INT: at most amax / 127), or <= max(|x| / 16, 2^(e-10)) (CMP_BYTE_FLOAT);
- * a group whose e is cut off at the upper end (amax above 1.6e38 or 1.5e38 only) saturates at its largest code instead.
+ * So |x - x'| <= 2^(e-1) (CMP_BYTE_INT: at most amax / 127 where e > -110), or <= max(|x| / 16, 2^(e-10)) (CMP_BYTE_FLOAT);
+ * a group whose e is cut off at the upper end (amax above 3.38e38 or 2.97e38 only) saturates at its largest code instead.
  * x' has at most eight significant bits: it is a bf16 number exactly.
  * The bytes, in one buffer aligned to 16:
  *    codes  rows * pitch, pitch = cols rounded up to 16; the padding behind a row is zero
@@ -368,7 +368,8 @@ int cmp_byte_linear_grad(int device, const cmp_byte_shape *shape, const void *d_
  *    dx = (du * gamma - (A + h * B) / count) / sqrt(var + eps),  A, B: sums of du * gamma, du * gamma * h over a group.
  * The statistics are those of the input itself, so the error of a code enters h divided by the group's deviation: a norm
  * whose deviation is not well above the steps 2^e of its checkpoint (groups of a few equal values, channels of very
- * different sizes in one scale group) is better kept as d_x.  The derivative of CMP_ACT_RELU at 0 is 0.  Sums run over fp32 or fp64 in an order that the sizes fix.
+ * different sizes in one scale group) is better kept as d_x.  The derivative of CMP_ACT_RELU at 0 is 0.  Sums run over
+ * fp32 or fp64 in an order that the sizes fix.
  * A NaN or an infinity in x spoils its group, as the formulas have it.  With batch or spatial 0 nothing is written
  * but zeros in dgamma and dbeta.  d_y must not overlap d_x, nor d_dx d_dy. */
 #define CMP_ACT_NONE 0u

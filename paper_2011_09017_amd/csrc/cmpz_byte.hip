@@ -3,7 +3,9 @@
 //
 // A thread takes 16 consecutive columns of a row: 128-bit accesses on both sides, and the group's largest
 // magnitude needs two, four or eight neighbouring lanes (DPP, no LDS).  Rows are dealt to threads in units of whole
-// groups, so that a group never crosses a wave.
+// groups, so that a group never crosses a wave.  Measured (a copy of 1 GiB reaches 5.16 TB/s): bf16 8192 x 8192
+// stored in 41.5 us (4.9 TB/s) and loaded in 32.6 (both tensors then fit the memory-side cache), fp32 387200 x 96 in
+// 35 to 38 us and 28.5; one row of 4096 in 2.0 and 1.8 us.
 #include "cmpz_byte.h"
 
 namespace cmpz {
@@ -121,13 +123,13 @@ void load_as(const ByteArgs &a, hipStream_t st)
         by_rows(a.rows, units, 4, [&](uint64_t r, uint32_t grid) {
             hipLaunchKernelGGL((k_byte_load_wide<F>), dim3(grid), dim3(kThreads), 0, st, a, r, units, d);
         });
-        return;
+    } else {
+        const uint32_t units = (uint32_t)(a.pitch / 16);
+        const FastDiv d = FastDiv::make(units);
+        by_rows(a.rows, units, 1, [&](uint64_t r, uint32_t grid) {
+            hipLaunchKernelGGL((k_byte_load<T, F>), dim3(grid), dim3(kThreads), 0, st, a, r, units, d);
+        });
     }
-    const uint32_t units = (uint32_t)(a.pitch / 16);
-    const FastDiv d = FastDiv::make(units);
-    by_rows(a.rows, units, 1, [&](uint64_t r, uint32_t grid) {
-        hipLaunchKernelGGL((k_byte_load<T, F>), dim3(grid), dim3(kThreads), 0, st, a, r, units, d);
-    });
 }
 
 }  // namespace

@@ -98,6 +98,7 @@ bool slab_plan(Plan *out, const NormArgs &a, uint32_t lanes)
     if (rows > kSlabRows) return false;
     p.rows_per = a.spatial;
     finish_plan(&p, a);
+    if (a.batch * p.chunks * p.threads > 1ull << 31) return false;        // a launch counts its threads with 32 bits
     *out = p;
     return true;
 }

@@ -18,8 +18,8 @@ typedef __bf16   bf16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x4  __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
 
-constexpr uint32_t kStep = 32;                 // rows of a stage: the reduction of one matrix instruction
-constexpr uint32_t kThreads = 256;             // four waves
+constexpr uint32_t kStep = 32;                 // rows of a stage: the reduction of two matrix instructions
+constexpr uint32_t kThreads = 256;             // four waves (the largest tile: eight)
 constexpr uint32_t kPad = 64;                  // behind a row in LDS: the four rows of a transposed read of 32 columns lie in
                                                // different banks
 
@@ -80,9 +80,9 @@ __device__ __forceinline__ void split8(f32x8 v, u32x4 *out)
     }
 }
 
-// Eight reduction rows of a column, as a matrix operand: lane l holds column l % 16, rows 8 * (l / 16) .. + 7.
-// `at`: the lane's address of row 8 * (l / 16) + (l % 16) / 4, column 4 * (l % 4); a group of 16 lanes reads four rows of
-// sixteen columns, which arrive transposed.
+// Eight reduction rows of a column, as a matrix operand: lane l holds column l % 32, rows 8 * (l / 32) .. + 7.
+// `at`: the lane's address of row 8 * (l / 32) + (l % 16) / 4, column 16 * (l / 16 % 2) + 4 * (l % 4); a group of 16 lanes
+// reads four rows of sixteen columns, which arrive transposed.
 template <uint32_t PITCH>
 __device__ __forceinline__ bf16x8 transposed(const uint8_t *at)
 {
@@ -404,8 +404,8 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void k_linear_grad(LinearGradArgs 
         step(odd, no, yes, t + 1);
     }
 
-    // ---- results: a lane holds column n = lane % 16 and four consecutive k of every 16 x 16; sixteen rows of dW at a
-    // time go through LDS, so that a row is stored by neighbouring lanes ----
+    // ---- results: a lane holds row n = lane % 32 of dW and four times four consecutive k of every 32 x 32; 32 rows at a time
+    // go through LDS, so that a row is stored by neighbouring lanes ----
     __syncthreads();
     float *rows = reinterpret_cast<float *>(s_all) + wave * (32u * RW);   // RW floats a row, RV vectors of four in it
     void *out = p.splits > 1 ? static_cast<void *>(a.work + (uint64_t)split * a.outs * a.cols) : a.dw;

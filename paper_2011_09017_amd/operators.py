@@ -192,6 +192,7 @@ def byte_linear_grad(dy: torch.Tensor, ck: ByteCheckpoint, bias: bool = False, d
 @lru_cache(maxsize=4096)
 def _norm_plan(batch: int, spatial: int, channels: int, groups: int, kind: int, act: str, eps: float):
     """(the C shape, bytes of the workspace): depend on sizes only and are read only."""
+    _refuse(not 0 <= groups < 1 << 32 or channels >= 1 << 32, f"group norm: {groups} groups of {channels} channels")   # fields of 32 bits
     shape = binding.cmp_norm_shape(batch, spatial, channels, groups, kind, _ACTS[act], eps)
     return shape, binding.cmp_group_norm_work(shape)
 

@@ -51,6 +51,25 @@ def test_library_refusals():
     assert grad(None, None) == grad(P, P) == grad(P, None, 0) == b.CMP_E_ARG
 
 
+def test_sizes_past_32_bits_are_refused():
+    """Fields of the C shape have 32 bits: what would wrap round to a legal size is refused."""
+    with pytest.raises(ValueError, match="groups"):
+        ops.group_norm(torch.empty(1, 8), (1 << 32) + 2)
+    with pytest.raises(ValueError, match="channels"):
+        ops.group_norm(torch.empty(0, (1 << 32) + 8), 2)
+    with pytest.raises(ValueError, match="groups"):
+        ops.group_norm(torch.empty(1, 8), -1)
+
+
+def test_the_plan_keeps_to_what_a_launch_can_count():
+    """2^21 samples of one position and 8192 channels: in segments of 64 channels they would be 2^28 workgroups, too many
+    threads for one launch; the workspace is that of two passes, with a record of totals per sample and group."""
+    shape = binding.cmp_norm_shape(1 << 21, 1, 8192, 128, binding.CMP_TYPE_BF, binding.CMP_ACT_NONE, 1e-5)
+    assert binding.cmp_group_norm_work(shape) >= (1 << 21) * (16 * 128 + 8 * 8192)
+    few = binding.cmp_norm_shape(1 << 10, 1, 8192, 128, binding.CMP_TYPE_BF, binding.CMP_ACT_NONE, 1e-5)
+    assert binding.cmp_group_norm_work(few) == (1 << 10) * 8 * 8192
+
+
 def test_formulas_against_differences():
     """The reference's gradients against differences of its forward pass (x' = x)."""
     gen = torch.Generator().manual_seed(0)
