@@ -3,6 +3,8 @@
 The hot path (pre-quantisation, 2D Lorenzo, outlier split, histogram, canonical
 Huffman, chunked bit-packing and the inverse) runs entirely in hand-written HIP
 kernels behind the C ABI declared in ``include/cmpz.h``; :mod:`.binding` is the
-argument-marshalling layer over it.  Importing this package does not load the
+argument-marshalling layer over it.  :mod:`.operators` holds other activations with eight
+bits per value and computes the backward pass of linear layers and group norm from that form;
+:mod:`.autograd` has hooks and layers over both.  Importing this package does not load the
 library; the first use of :mod:`.binding` does, and fails loudly if it is absent.
 """

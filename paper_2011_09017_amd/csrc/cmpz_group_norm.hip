@@ -11,6 +11,11 @@
 // k_norm_grad_slab).  Otherwise there are two passes: a workgroup takes a range of positions with all their channels.
 // In both a thread takes eight neighbouring channels (128-bit accesses whatever a group's width is) of every rp-th
 // position; sums are kept per channel and thread and joined per channel, then per group, in LDS.
+//
+// Measured on bf16 with int8 codes, SiLU: 256 x 12544 x 64 in 8 groups (411 MB a tensor, copies run at 5.16 TB/s): forward sums
+// 104 us (3.9 TB/s), apply 215 (1031 MB in all, 4.8); backward sums 176 (3.5: the sigmoid and the codes' expansion on 16
+// values a lane beside 48 bytes of loads), apply 202 (5.1); counters show no byte read twice.  One pass, 256 x 49 x 512 fp32:
+// 17 and 23 us (3.7 and 3.2 TB/s), two waves to a SIMD for their registers; one sample of 16 x 16 x 320: 6.0 us, latency.
 #include "cmpz_byte.h"
 
 #include <type_traits>

@@ -4,6 +4,13 @@
 // The codes are expanded to bf16 on their way into LDS, which is exact (the scales are powers of two), and the sums
 // run in fp32 in the matrix units.  dY in bf16 enters as it is; fp16 and fp32 are split by truncation into two
 // or three bf16 terms that add up to the value exactly, at two or three times the matrix work.
+//
+// Both operands are reduced along their rows, so both are read transposed from LDS.  Measured, rows x cols x outs of
+// 8192 x 4096 x 4096 on random values: int8 with bf16 252 us (1.09 PFLOP/s), e4m3 226, fp16 450 and fp32 660 (two and three
+// terms); 16384 x 4096 x 8192 e4m3 877 us (1.25 PFLOP/s); 8192^3 as A^T B from bf16 in memory the library reaches 1.12.
+// A stage of 32 rows takes 1.17 us at 256 x 256, of which the matrix instructions are busy for half; beside them lie the
+// expansion (int8: 12 % over e4m3) and 3.4 reads of the operands through eight L2 caches (340 MB, 1.35 TB/s: no bound).
+// Operands of zeros take 219 us: part of the rest is power.
 #include "cmpz_byte.h"
 
 #include <cmath>
@@ -447,7 +454,8 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void k_linear_grad(LinearGradArgs 
 }
 
 // Fewer than eight outputs (a gate, a small head), or no columns at all: too narrow for the matrix tiles.  A thread takes
-// four columns and eight outputs over a range of rows, in fp32; bound by reading the codes once.
+// four columns and eight outputs over a range of rows, in fp32; bound by reading the codes once and, for few of them, by
+// latency.
 template <uint32_t T, uint32_t F>
 __global__ __launch_bounds__(kThreads) void k_linear_grad_few(LinearGradArgs a, Plan p)
 {
