@@ -8,7 +8,7 @@
 // Both operands are reduced along their rows, so both are read transposed from LDS.  Measured, rows x cols x outs of
 // 8192 x 4096 x 4096 on random values: int8 with bf16 252 us (1.09 PFLOP/s), e4m3 226, fp16 450 and fp32 660 (two and three
 // terms); 16384 x 4096 x 8192 e4m3 877 us (1.25 PFLOP/s); 8192^3 as A^T B from bf16 in memory the library reaches 1.12.
-// A stage of 32 rows takes 1.17 us at 256 x 256, of which the matrix instructions are busy for half; beside them lie the
+// A stage of 32 rows takes 0.98 us at 256 x 256, of which the matrix instructions are busy for half; beside them lie the
 // expansion (int8: 12 % over e4m3) and 3.4 reads of the operands through eight L2 caches (340 MB, 1.35 TB/s: no bound).
 // Operands of zeros take 219 us: part of the rest is power.
 #include "cmpz_byte.h"
@@ -561,12 +561,12 @@ JoinJob join_job(const float *w, uint32_t count, uint64_t n, void *out)
 
 // Tiles of dW that a workgroup may take, its sets of waves, how many such workgroups a CU holds, and what a stage (32 rows
 // of each set) takes with w of them on it, in ns, for t terms: a0 + a1 * t + (b0 + b1 * t) * w.  Fitted to 8192 and 16384 rows, all
-// CUs busy (ns measured / fitted for bf16, fp16, fp32): 256 x 256: 1190 / 1170, 1900 / 1860, 2550 / 2550; 128 x 128: 707 / 707, 1205 /
+// CUs busy (ns measured / fitted for bf16, fp16, fp32): 256 x 256: 980 / 975, 1740 / 1760, 2550 / 2545; 128 x 128: 707 / 707, 1205 /
 // 1199, 1692 / 1691; 64 x 256: 884 / 882, 1210 / 1254, 1631 / 1626; 64 x 64, two of them: 801 / 800, 1120 / 1120, one: 564 / 560, fp32
 // 818 / 820.  With one set, two workgroups to a CU, the middle two take 4 to 15 % longer and leave twice the partial sums
 // (8192 x 1024 x 1024 bf16: 42 us where this takes 38; 200704 x 256 x 64 fp32: 43 and 37).
 struct Tile { uint32_t n, k, sets, resident; double a0, a1, b0, b1; };
-constexpr Tile kTiles[] = {{256, 256, 1, 1, 480, 690, 0, 0}, {128, 128, 2, 1, 215, 492, 0, 0}, {64, 256, 2, 1, 510, 372, 0, 0},
+constexpr Tile kTiles[] = {{256, 256, 1, 1, 190, 785, 0, 0}, {128, 128, 2, 1, 215, 492, 0, 0}, {64, 256, 2, 1, 510, 372, 0, 0},
                            {64, 64, 2, 2, 380, -60, 50, 190}};
 constexpr int kTileCount = 4, kFewOutputs = kTileCount;
 
