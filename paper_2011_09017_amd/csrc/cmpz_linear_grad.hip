@@ -454,13 +454,16 @@ __global__ __launch_bounds__(64 * WN * WK * SETS, 2) void k_linear_grad(LinearGr
         for (int k = 0; k < 8; ++k) s[threadIdx.x * 8u + k] = sum_b[k];
         __syncthreads();
         float *part_b = a.work + (p.splits > 1 ? (uint64_t)p.splits * a.outs * a.cols : 0) + (uint64_t)(split * p.sharers + tk) * a.outs;
-        if (threadIdx.x < VY && n0 + cy < a.outs) {
-            for (int k = 0; k < 8 && ny + k < a.outs; ++k) {
-                if (ny + k < n_first || ny + k < n0 + cy) continue;      // a vector moved back shares columns with the one before it
+        static_assert(SETS * kThreads >= TN, "a thread for every column");
+        if (threadIdx.x < TN) {                                           // a column each: vector threadIdx.x / 8 of the row
+            const uint32_t from = n0 + (threadIdx.x & ~7u), n = (from + 8 > a.outs ? a.outs - 8 : from) + (threadIdx.x & 7u);
+            // a vector moved back shares columns with the one before it, a last tile that starts earlier with the tile before
+            if (from < a.outs && n >= from && n >= n_first) {
                 float v = 0.0f;
-                for (uint32_t r = 0; r < SETS * kThreads / VY; ++r) v += s[(r * VY + tid) * 8u + k];
-                if (p.parts_b > 1) part_b[ny + k] = v;
-                else put(a.db, ny + k, a.out_type, v, a.accumulate);
+#pragma unroll 8
+                for (uint32_t r = 0; r < SETS * kThreads / VY; ++r) v += s[r * TN + threadIdx.x];
+                if (p.parts_b > 1) part_b[n] = v;
+                else put(a.db, n, a.out_type, v, a.accumulate);
             }
         }
     }
