@@ -14,7 +14,9 @@ not fp32 4-D CUDA tensors, small tensors and shapes the stack does not take are 
 
 What that codec does not take or does not shrink (bf16 and fp16, dense activations, channels last) can be held with
 eight bits per value instead: :class:`ByteCheckpoints` are hooks of the same kind over byte checkpoints, and
-:func:`linear` and :func:`group_norm` are layers whose backward pass reads the eight-bit form itself.
+:func:`linear` and :func:`group_norm` are layers whose backward pass reads the eight-bit form itself.  All of these can be
+captured into a graph; as with any layer of torch, no eager graph of the same parameters may be alive while
+``backward()`` is captured.
 """
 from __future__ import annotations
 

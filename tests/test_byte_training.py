@@ -311,6 +311,46 @@ def test_replays_from_a_graph():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("frozen", [False, True])
+def test_layers_replay_from_a_graph(dtype, frozen):
+    """A block of the layers, forward and backward through autograd, captured once; every replay on changed inputs, with
+    eager calls of the same block between, gives the eager results.  frozen: only the biases of the linear layers learn."""
+    p = _block_parameters(dtype)
+    learn = [p[3], p[7]] if frozen else p
+    if frozen:
+        for k in (0, 1, 2, 4, 5, 6):
+            p[k].requires_grad_(False)
+    gen = torch.Generator().manual_seed(19)
+    sets = [[torch.randn(6, 1000, 64, generator=gen).to(dtype).to(DEV) for _ in range(2)] for _ in range(3)]
+
+    def step(x, dy):
+        x = x.detach().requires_grad_()
+        y = _block(x, p, "int8")
+        return [y.detach(), *torch.autograd.grad(y, [x, *learn], dy)]
+
+    want = [[t.clone() for t in step(*s)] for s in sets]
+    ins = [t.clone() for t in sets[0]]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(*ins)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        outs = step(*ins)
+    for v in (1, 2, 0, 1):
+        for a, s in zip(ins, sets[v]):
+            a.copy_(s)
+        g.replay()
+        torch.cuda.synchronize()
+        for t, u in zip(outs, want[v]):
+            assert torch.equal(t, u)
+        step(*sets[(v + 1) % 3])
+        torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
 def test_two_streams_at_once():
     """The same calls on two streams, their buffers apart: the results of each alone."""
     gen = torch.Generator().manual_seed(17)
