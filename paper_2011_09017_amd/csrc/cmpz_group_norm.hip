@@ -78,7 +78,8 @@ uint32_t lcm(uint32_t x, uint32_t y)
 
 // The smallest segment is a multiple of eight channels, of a group and, where codes are written, of a quantisation group
 // (or all channels).  It grows to 128 bytes of a position, and below that there is no slab: with 64 bytes the backward
-// pass of 128 x 784 x 512 bf16 took 192 us where two passes take 93.  Small segments, down to a single wave, keep
+// pass of 128 x 784 x 512 bf16 took 192 us where two passes take 93.  It grows to 192 vectors too, three full waves: 4096 x 16 x
+// 512 bf16 took 75 and 103 us with 128 and 54 and 85 with 256, but 256 x 49 x 512 fp32 backward 25 with 196 and 32 with 392.  Small segments, down to a single wave, keep
 // all of a CU's registers busy with loads (256 x 7 x 7 x 512 fp32, both directions: 42 us, with 1024 vectors to a segment 80).
 bool slab_plan(Plan *out, const NormArgs &a, uint32_t lanes)
 {
@@ -91,7 +92,7 @@ bool slab_plan(Plan *out, const NormArgs &a, uint32_t lanes)
     auto fits = [&](uint32_t nv) { return (uint64_t)nv * a.spatial <= most && nv <= kMaxThreads; };
     if (!fits(unit)) return false;
     p.nv = unit;
-    while (p.nv + unit <= all && fits(p.nv + unit) && p.nv * 8 * type_bytes(a.type) < 128) p.nv += unit;
+    while (p.nv + unit <= all && fits(p.nv + unit) && (p.nv * 8 * type_bytes(a.type) < 128 || (uint64_t)p.nv * a.spatial < 192)) p.nv += unit;
     if (p.nv < all && p.nv * 8 * type_bytes(a.type) < 128) return false;
     p.chunks = (all + p.nv - 1) / p.nv;
     // Positions per thread: as many as it can hold, so that a CU has most bytes in flight; one where all threads fit the
@@ -164,13 +165,40 @@ __device__ __forceinline__ void join_channels(V *s, const V (&v)[8], const V (&w
     __syncthreads();
 }
 
-// Sum over a group's channels of f(channel of the segment), by one wave; g counts from the segment's first group.
+// Lanes that add up `items` values: a whole wave, or for few a power of two of it, so that a wave takes several groups at once
+// (65536 x 1 x 512 in 32 groups, forward: 880 us with a wave to a group, 140 so; 64 x 3136 x 256 in 256: 117 and 83).
+__device__ __forceinline__ uint32_t lanes_of(uint32_t items)
+{
+    uint32_t w = 64u;
+    while (w > 1u && w / 2u >= items) w >>= 1;
+    return w;
+}
+__device__ __forceinline__ double lanes_sum(double v, uint32_t w)
+{
+    if (w == 64u) return wave_sum(v);
+    for (uint32_t k = w >> 1; k; k >>= 1) v += __shfl_xor(v, (int)k);
+    return v;
+}
+
+// For each of `groups` groups, w lanes to one: take(group, lane of the w, mine).  Lanes behind the last group take it once more
+// (take's sums cross lanes); `mine`: this lane has the group's result.
 template <class FN>
-__device__ __forceinline__ double group_total(uint32_t g, uint32_t per, FN f)
+__device__ __forceinline__ void each_group(uint32_t groups, uint32_t w, FN take)
+{
+    const uint32_t at_once = 64u / w, lane = threadIdx.x & 63u;
+    for (uint32_t g0 = (threadIdx.x >> 6) * at_once; g0 < groups; g0 += (blockDim.x >> 6) * at_once) {
+        const uint32_t g = g0 + lane / w;
+        take(g < groups ? g : groups - 1u, lane & (w - 1u), g < groups && (lane & (w - 1u)) == 0);
+    }
+}
+
+// Sum over a group's channels of f(channel of the segment), by w lanes; g counts from the segment's first group.
+template <class FN>
+__device__ __forceinline__ double group_total(uint32_t g, uint32_t per, uint32_t sub, uint32_t w, FN f)
 {
     double t = 0.0;
-    for (uint32_t c = threadIdx.x & 63u; c < per; c += 64u) t += f(g * per + c);
-    return wave_sum(t);
+    for (uint32_t c = sub; c < per; c += w) t += f(g * per + c);
+    return lanes_sum(t, w);
 }
 
 // ---- forward ------------------------------------------------------------------------------------------
@@ -187,14 +215,12 @@ __device__ __forceinline__ void add_moments(f32x8 v, double (&s1)[8], double (&s
     }
 }
 
-// Totals of the workgroup for each of `groups` groups of its segment: give(g, sum, sum of squares) by the first lane
-// of a wave.  Groups of eight channels and more: a vector lies in one or two of them, and its channels are added up to
+// Totals of the workgroup for each of `groups` groups of its segment: give(g, sum, sum of squares) by one lane.  Groups of eight channels and more: a vector lies in one or two of them, and its channels are added up to
 // these before LDS (32 bytes a thread instead of 128, which would leave a CU two workgroups).
 template <class FN>
 __device__ __forceinline__ void join_moments(double *s, double (&s1)[8], double (&s2)[8], uint32_t groups, const Plan &p, const Place &q,
                                              uint32_t first, FN give)
 {
-    const uint32_t wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63u;
     if (p.per >= 8) {
         const uint32_t c0 = q.c - first, g0 = p.div_per.div(c0), cut = (g0 + 1u) * p.per - c0;   // channels in the first of the two
         double t1 = 0.0, t2 = 0.0, u1 = 0.0, u2 = 0.0;
@@ -206,27 +232,29 @@ __device__ __forceinline__ void join_moments(double *s, double (&s1)[8], double 
         double *o = s + 4u * threadIdx.x;
         o[0] = t1; o[1] = t2; o[2] = u1; o[3] = u2;
         __syncthreads();
-        for (uint32_t g = wave; g < groups; g += waves) {
+        const uint32_t w = lanes_of((p.per / 8u + 2u) * p.rp);
+        each_group(groups, w, [&](uint32_t g, uint32_t sub, bool mine) {
             const uint32_t v0 = g * p.per / 8u, nv = ((g + 1u) * p.per - 1u) / 8u - v0 + 1u, items = nv * p.rp;
-            t1 = t2 = 0.0;
-            for (uint32_t i = lane; i < items; i += 64u) {
+            double a1 = 0.0, a2 = 0.0;
+            for (uint32_t i = sub; i < items; i += w) {
                 const uint32_t r = i / nv, v = v0 + (i - r * nv);
                 const double *in = s + 4u * (r * p.nv + v) + (8u * v < g * p.per ? 2u : 0u);
-                t1 += in[0];
-                t2 += in[1];
+                a1 += in[0];
+                a2 += in[1];
             }
-            t1 = wave_sum(t1);
-            t2 = wave_sum(t2);
-            if (lane == 0) give(g, t1, t2);
-        }
+            a1 = lanes_sum(a1, w);
+            a2 = lanes_sum(a2, w);
+            if (mine) give(g, a1, a2);
+        });
     } else {
         join_channels(s, s1, s2, p);
         const double *u = s + blockDim.x * 8u;
-        for (uint32_t g = wave; g < groups; g += waves) {
-            const double t1 = group_total(g, p.per, [&](uint32_t c) { return s[c]; });
-            const double t2 = group_total(g, p.per, [&](uint32_t c) { return u[c]; });
-            if (lane == 0) give(g, t1, t2);
-        }
+        const uint32_t w = lanes_of(p.per);
+        each_group(groups, w, [&](uint32_t g, uint32_t sub, bool mine) {
+            const double a1 = group_total(g, p.per, sub, w, [&](uint32_t c) { return s[c]; });
+            const double a2 = group_total(g, p.per, sub, w, [&](uint32_t c) { return u[c]; });
+            if (mine) give(g, a1, a2);
+        });
     }
 }
 
@@ -628,7 +656,8 @@ __device__ __forceinline__ void pick_totals(const double *s, const NormArgs &a, 
 }
 
 // dbeta and dgamma of sixteen channels: the sums of `records` workgroups or samples, in a fixed order.
-__device__ __forceinline__ void join_parameters(double *s, const NormArgs &a, const float *chan, uint64_t records, uint32_t block)
+__device__ __forceinline__ void join_parameters(double *s, const NormArgs &a, const float *chan, uint64_t records, uint32_t block,
+                                                float *dbeta, float *dgamma)
 {
     const uint32_t c = block * 16u + (threadIdx.x & 15u), parts = blockDim.x >> 4;
     double t[2] = {0.0, 0.0};
@@ -640,7 +669,7 @@ __device__ __forceinline__ void join_parameters(double *s, const NormArgs &a, co
         }
     }
     for (int which = 0; which < 2; ++which) {
-        float *out = which ? a.dgamma : a.dbeta;
+        float *out = which ? dgamma : dbeta;
         __syncthreads();
         s[threadIdx.x] = t[which];
         __syncthreads();
@@ -653,10 +682,23 @@ __device__ __forceinline__ void join_parameters(double *s, const NormArgs &a, co
     }
 }
 
-__global__ __launch_bounds__(kMaxThreads) void k_norm_parameters(NormArgs a, uint64_t records)
+// blocks: workgroups for all channels.  With `to` a workgroup joins one of several ranges of records to a record there.
+__global__ __launch_bounds__(kMaxThreads) void k_norm_parameters(NormArgs a, const float *chan, uint64_t records, uint64_t range,
+                                                                 uint32_t blocks, float *to)
 {
     extern __shared__ double s_sum[];
-    join_parameters(s_sum, a, static_cast<const float *>(a.work), records, blockIdx.x);
+    const uint32_t r = blockIdx.x / blocks, block = blockIdx.x - r * blocks;
+    const uint64_t beg = r * range, n = records - beg < range ? records - beg : range;
+    float *out = to + 2ull * r * a.channels;
+    join_parameters(s_sum, a, chan + 2 * beg * a.channels, n, block, to ? out : a.dbeta, to ? out + a.channels : a.dgamma);
+}
+
+// Ranges that the records of many samples are joined in first, so that more than the few workgroups of the channels
+// read them (100000 x 1 x 40, backward: 634 us with one step, 136 with two; 3000 x 9 x 256: 39.9 and 28.6); 1: a second launch would cost more.
+uint32_t parameter_ranges(const NormArgs &a, uint64_t records)
+{
+    const uint32_t blocks = (a.channels + 15) / 16;
+    return records < 2048 || blocks >= 256 ? 1 : 512 / blocks;
 }
 
 template <uint32_t T, uint32_t S, uint32_t ACT, bool ONE>
@@ -692,7 +734,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_slab(NormArgs a, Plan
     double *tot = s_sum + 8u * blockDim.x + 4u * p.nv;
     const float *s2 = s + blockDim.x * 8u, *sg = put_gamma(s + blockDim.x * 16u, p, q, ch);
     join_channels(s, sp, sq, p);
-    const uint32_t groups = (end - first) / p.per, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const uint32_t groups = (end - first) / p.per, w = lanes_of(p.per);
     for (uint32_t c = threadIdx.x; c < end - first; c += blockDim.x) {
         if (a.batch == 1) {
             if (a.dbeta) a.dbeta[first + c] = s[c];
@@ -703,11 +745,11 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_slab(NormArgs a, Plan
             chan[a.channels] = s2[c];
         }
     }
-    for (uint32_t g = wave; g < groups; g += waves) {
-        const double t1 = group_total(g, p.per, [&](uint32_t c) { return (double)s[c] * (double)sg[c]; });
-        const double t2 = group_total(g, p.per, [&](uint32_t c) { return (double)s2[c] * (double)sg[c]; });
-        if ((threadIdx.x & 63u) == 0) { tot[2 * g] = t1; tot[2 * g + 1] = t2; }
-    }
+    each_group(groups, w, [&](uint32_t g, uint32_t sub, bool mine) {
+        const double t1 = group_total(g, p.per, sub, w, [&](uint32_t c) { return (double)s[c] * (double)sg[c]; });
+        const double t2 = group_total(g, p.per, sub, w, [&](uint32_t c) { return (double)s2[c] * (double)sg[c]; });
+        if (mine) { tot[2 * g] = t1; tot[2 * g + 1] = t2; }
+    });
     __syncthreads();
     float ga[ONE ? 1 : 8], gb[ONE ? 1 : 8];
     pick_totals<ONE>(tot, a, p, q, first, ga, gb);
@@ -768,19 +810,19 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_sums(NormArgs a, Plan
     float *s = reinterpret_cast<float *>(s_sum);
     const float *s2 = s + blockDim.x * 8u, *sg = put_gamma(s + blockDim.x * 16u, p, q, ch);
     join_channels(s, sp, sq, p);
-    const uint32_t wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const uint32_t w = lanes_of(p.per);
     double *part = static_cast<double *>(a.work);
     float *chan = reinterpret_cast<float *>(part + 2ull * a.batch * a.groups * p.chunks) + 2ull * blockIdx.x * a.channels;
     for (uint32_t c = threadIdx.x; c < a.channels; c += blockDim.x) {
         chan[c] = s[c];
         chan[a.channels + c] = s2[c];
     }
-    for (uint32_t g = wave; g < a.groups; g += waves) {
-        const double t1 = group_total(g, p.per, [&](uint32_t c) { return (double)s[c] * (double)sg[c]; });
-        const double t2 = group_total(g, p.per, [&](uint32_t c) { return (double)s2[c] * (double)sg[c]; });
+    each_group(a.groups, w, [&](uint32_t g, uint32_t sub, bool mine) {
+        const double t1 = group_total(g, p.per, sub, w, [&](uint32_t c) { return (double)s[c] * (double)sg[c]; });
+        const double t2 = group_total(g, p.per, sub, w, [&](uint32_t c) { return (double)s2[c] * (double)sg[c]; });
         double *o = part + (((uint64_t)q.n * a.groups + g) * p.chunks + q.chunk) * 2;
-        if ((threadIdx.x & 63u) == 0) { o[0] = t1; o[1] = t2; }
-    }
+        if (mine) { o[0] = t1; o[1] = t2; }
+    });
 }
 
 // Between the two passes: the totals A and B of every sample and group, and the parameters' gradients.
@@ -790,7 +832,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_join(NormArgs a, Plan
     const double *part = static_cast<const double *>(a.work);
     if (blockIdx.x < param_blocks) {
         join_parameters(s_sum, a, reinterpret_cast<const float *>(part + 2ull * a.batch * a.groups * p.chunks),
-                        a.spatial ? a.batch * p.chunks : 0, blockIdx.x);
+                        a.spatial ? a.batch * p.chunks : 0, blockIdx.x, a.dbeta, a.dgamma);
         return;
     }
     const uint64_t step = (gridDim.x - param_blocks) * 16ull;
@@ -863,7 +905,20 @@ void backward_as(const NormArgs &a, hipStream_t st)
     if (a.batch && slab_plan(&p, a, 1)) {
         hipLaunchKernelGGL((k_norm_grad_slab<T, S, ACT, ONE>), dim3((uint32_t)(a.batch * p.chunks)), dim3(p.threads),
                            lds_bytes(p, 64, p.nv * 8u / p.per, true) + 32 * p.nv, st, a, p);
-        if (params && a.batch > 1) hipLaunchKernelGGL(k_norm_parameters, dim3(params), dim3(1024), 8 * 1024, st, a, a.batch);
+        if (!params || a.batch == 1) return;
+        const float *chan = static_cast<const float *>(a.work);
+        uint64_t records = a.batch;
+        const uint32_t ranges = parameter_ranges(a, records);
+        if (ranges > 1) {
+            const uint64_t range = (records + ranges - 1) / ranges, used = (records + range - 1) / range;
+            float *to = static_cast<float *>(a.work) + 2 * records * a.channels;
+            hipLaunchKernelGGL(k_norm_parameters, dim3((uint32_t)used * params), dim3(kMaxThreads), 8 * kMaxThreads, st, a, chan, records, range,
+                               params, to);
+            chan = to;
+            records = used;
+        }
+        hipLaunchKernelGGL(k_norm_parameters, dim3(params), dim3(kMaxThreads), 8 * kMaxThreads, st, a, chan, records, records, params,
+                           static_cast<float *>(nullptr));
         return;
     }
     p = two_pass_plan(a, 1);
@@ -925,7 +980,7 @@ uint64_t group_norm_work(const NormArgs &a)
     for (uint32_t lanes : {1u, 4u, 8u, 16u}) {
         Plan p;
         uint64_t bytes;
-        if (slab_plan(&p, a, lanes)) bytes = lanes == 1u && a.batch > 1 ? 8ull * a.batch * a.channels : 0;    // sums of every sample
+        if (slab_plan(&p, a, lanes)) bytes = lanes == 1u && a.batch > 1 ? 8ull * (a.batch + parameter_ranges(a, a.batch)) * a.channels : 0;   // sums of every sample
         else bytes = records_bytes(a, two_pass_plan(a, lanes), lanes == 1u) + 16ull * a.batch * a.groups;
         if (bytes > most) most = bytes;
     }

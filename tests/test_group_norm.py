@@ -62,12 +62,12 @@ def test_sizes_past_32_bits_are_refused():
 
 
 def test_the_plan_keeps_to_what_a_launch_can_count():
-    """2^21 samples of one position and 8192 channels: in segments of 64 channels they would be 2^28 workgroups, too many
-    threads for one launch; the workspace is that of two passes, with a record of totals per sample and group."""
+    """2^21 samples of one position and 8192 channels: in segments of 1536 channels they would be 6 * 2^21 workgroups of 192, too
+    many threads for one launch; the workspace is that of two passes, with a record of totals per sample and group."""
     shape = binding.cmp_norm_shape(1 << 21, 1, 8192, 128, binding.CMP_TYPE_BF, binding.CMP_ACT_NONE, 1e-5)
     assert binding.cmp_group_norm_work(shape) >= (1 << 21) * (16 * 128 + 8 * 8192)
     few = binding.cmp_norm_shape(1 << 10, 1, 8192, 128, binding.CMP_TYPE_BF, binding.CMP_ACT_NONE, 1e-5)
-    assert binding.cmp_group_norm_work(few) == (1 << 10) * 8 * 8192
+    assert (1 << 10) * 8 * 8192 <= binding.cmp_group_norm_work(few) < (1 << 10) * (16 * 128 + 8 * 8192)       # one pass
 
 
 def test_formulas_against_differences():
@@ -179,6 +179,16 @@ def test_both_directions(batch, spatial, channels, groups, dtype, act, save, gro
     assert torch.equal(again[0], y) and torch.equal(again[1], stats)
     for p, q in zip(ops.group_norm_grad(dy, x if ck is None else ck, stats, groups, w, b, act), (dx, dw, db)):
         assert torch.equal(p, q)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch,spatial,channels,groups", [(5000, 1, 40, 5), (2100, 2, 520, 130), (3000, 4, 96, 3), (2049, 7, 16, 16),
+                                                           (2048, 16, 64, 2), (4097, 1, 4104, 1), (2500, 1, 7, 7)])
+@pytest.mark.parametrize("dtype,act,save,group", [(torch.bfloat16, "silu", "int8", 32), (torch.float32, "relu", None, 64),
+                                                  (torch.float16, "none", "e4m3", 128)])
+def test_many_samples(batch, spatial, channels, groups, dtype, act, save, group):
+    """The sums of the parameters are joined in two steps, groups of few values by a part of a wave."""
+    test_both_directions(batch, spatial, channels, groups, dtype, act, save, group)
 
 
 @pytest.mark.gpu
