@@ -135,7 +135,8 @@ __device__ __forceinline__ void put4(void *p, uint64_t i, uint32_t type, f32x4 v
         if (k < left) put(p, i + k, type, v[k], accumulate);
 }
 
-struct Plan { uint32_t tiles_n, tiles_k, splits, rows_per, sharers, parts_b; };     // sharers: tiles that share a range's sum of db; parts_b: its parts
+// sharers: tiles that share a range's sum of db; parts_b: its parts; few_log: for few outputs, log2 of the threads of a row
+struct Plan { uint32_t tiles_n, tiles_k, splits, rows_per, sharers, parts_b, few_log; };
 
 // Eight values of dY as they lie in memory.
 template <uint32_t T> struct Raw { u32x4 w[T == kTypeF32 ? 2 : 1]; };
@@ -470,50 +471,94 @@ __global__ __launch_bounds__(64 * WN * WK * SETS, 2) void k_linear_grad(LinearGr
 }
 
 // Fewer than eight outputs (a gate, a small head), or no columns at all: too narrow for the matrix tiles.  A thread takes
-// four columns and eight outputs over a range of rows, in fp32; bound by reading the codes once and, for few of them, by
-// latency.
-template <uint32_t T, uint32_t F>
+// four columns and NO outputs of every parts-th row of a range, in fp32; a row takes 2^few_log threads, and the parts meet in LDS.
+// Loads are unconditional (what does not exist repeats its neighbour), so that those of four rows are under way at once:
+// 8192 x 4096 x 1 bf16 with db 20 us, 500000 x 8 x 2 fp32 28 (with a thread to four columns of all rows of a range, and loads
+// behind branches, 54 and 356); latency and the join, the codes alone are 6.6 us of reading.
+template <uint32_t T, uint32_t F, int NO>
 __global__ __launch_bounds__(kThreads) void k_linear_grad_few(LinearGradArgs a, Plan p)
 {
     typedef typename ElemOf<T>::type E;
+    __shared__ f32x4 s[kThreads];
     uint32_t b = blockIdx.x;
     const uint32_t tn = b % p.tiles_n; b /= p.tiles_n;
     const uint32_t tk = b % p.tiles_k, split = b / p.tiles_k;
-    const uint32_t n0 = tn * 8u, k0 = (tk * kThreads + threadIdx.x) * 4u;
+    const uint32_t wide = 1u << p.few_log, parts = kThreads >> p.few_log, slot = threadIdx.x & (wide - 1u), part = threadIdx.x >> p.few_log;
+    const uint32_t n0 = tn * NO, k0 = (tk * wide + slot) * 4u;
     const uint32_t m_beg = split * p.rows_per, m_end = a.rows - m_beg < p.rows_per ? a.rows : m_beg + p.rows_per;
-    const int n = (int)(a.outs - n0);
-    const bool mine = k0 < a.cols, with_db = a.db && tk == 0 && threadIdx.x == 0;
-    f32x4 acc[8];
-    f32x8 sum = {0, 0, 0, 0, 0, 0, 0, 0};
+    const int n = a.outs - n0 < NO ? (int)(a.outs - n0) : NO;
+    const bool mine = k0 < a.cols && part == 0;
+    const uint32_t k_read = k0 < a.cols ? k0 : 0u;
+    f32x4 acc[NO];
+    float sum[NO];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] = f32x4{0, 0, 0, 0};
-    if (mine || with_db) {
-        const E *dy = static_cast<const E *>(a.dy) + n0;
+    for (int j = 0; j < NO; ++j) {
+        acc[j] = f32x4{0, 0, 0, 0};
+        sum[j] = 0.0f;
+    }
+    const E *dy = static_cast<const E *>(a.dy) + n0;
+    auto values = [&](uint32_t m, float (&y)[NO]) {
+#pragma unroll
+        for (int j = 0; j < NO; ++j) {
+            y[j] = (float)dy[(uint64_t)m * a.ld_dy + (j < n ? j : n - 1)];
+            sum[j] += y[j];
+        }
+    };
+    if (a.cols) {
 #pragma unroll 4
-        for (uint32_t m = m_beg; m < m_end; ++m) {
-            const f32x8 y = load8<T>(dy + (uint64_t)m * a.ld_dy, n);
-            sum += y;
-            if (mine) {
-                const f32x4 x = decode4<F>(*reinterpret_cast<const uint32_t *>(a.codes + (uint64_t)m * a.pitch + k0),
-                                           scale_of(a.exps[(uint64_t)m * a.ngroups + (k0 >> a.gshift)]));
+        for (uint32_t m = m_beg + part; m < m_end; m += parts) {
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(a.codes + (uint64_t)m * a.pitch + k_read);
+            const uint32_t e = a.exps[(uint64_t)m * a.ngroups + (k_read >> a.gshift)];
+            float y[NO];
+            values(m, y);
+            const f32x4 x = decode4<F>(w, scale_of(e));
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
+            for (int j = 0; j < NO; ++j)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[j][q] = __builtin_fmaf(y[j], x[q], acc[j][q]);
-            }
+                for (int q = 0; q < 4; ++q) acc[j][q] = __builtin_fmaf(y[j], x[q], acc[j][q]);
+        }
+    } else {
+#pragma unroll 4
+        for (uint32_t m = m_beg + part; m < m_end; m += parts) {
+            float y[NO];
+            values(m, y);
         }
     }
     void *out = p.splits > 1 ? static_cast<void *>(a.work + (uint64_t)split * a.outs * a.cols) : a.dw;
     float *part_b = a.work + (uint64_t)p.splits * a.outs * a.cols + (uint64_t)split * a.outs;
+    const bool with_db = a.db && tk == 0;                                 // uniform
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        if (j >= n) continue;
+    for (int j = 0; j < NO; ++j) {
+        if (j >= n) break;
+        if (parts > 1 && a.cols) {
+            __syncthreads();
+            s[threadIdx.x] = acc[j];
+            __syncthreads();
+            if (part == 0) {
+#pragma unroll 4
+                for (uint32_t r = 1; r < parts; ++r) acc[j] += s[r * wide + slot];
+            }
+        }
         if (mine)
             put4(out, (uint64_t)(n0 + j) * a.cols + k0, p.splits > 1 ? kTypeF32 : a.out_type, acc[j], p.splits > 1 ? 0u : a.accumulate,
                  a.cols - k0 < 4 ? (int)(a.cols - k0) : 4);
-        if (with_db) {
-            if (p.splits > 1) part_b[n0 + j] = sum[j];
-            else put(a.db, n0 + j, a.out_type, sum[j], a.accumulate);
+    }
+    if (with_db) {
+        float *sb = reinterpret_cast<float *>(s);
+#pragma unroll
+        for (int j = 0; j < NO; ++j) {
+            if (j >= n) break;
+            if (parts > 1) {
+                __syncthreads();
+                if (slot == 0) sb[part] = sum[j];
+                __syncthreads();
+            }
+            if (threadIdx.x == 0) {
+#pragma unroll 8
+                for (uint32_t r = 1; r < parts; ++r) sum[j] += sb[r];
+                if (p.splits > 1) part_b[n0 + j] = sum[j];
+                else put(a.db, n0 + j, a.out_type, sum[j], a.accumulate);
+            }
         }
     }
 }
@@ -597,8 +642,10 @@ Choice choose(uint64_t rows, uint64_t cols, uint64_t outs, uint32_t type)
     const uint64_t steps = (rows + kStep - 1) / kStep;
     Choice c{kFewOutputs, {}};
     uint64_t splits = 1;
-    uint32_t tile_n = 8, tile_k = 4 * kThreads;
+    uint32_t tile_n = 8, tile_k = 4;
+    c.plan.few_log = 0;
     if (few_outputs(cols, outs)) {
+        for (; tile_k < 256 && tile_k < cols; tile_k *= 2) ++c.plan.few_log;
         const uint64_t tiles = ((outs + 7) / 8) * ((cols + tile_k - 1) / tile_k + (cols == 0));
         splits = tiles && tiles < 1024 ? 1024 / tiles : 1;
         if (splits > (steps + 1) / 2) splits = (steps + 1) / 2;           // no fewer than two stages each
@@ -643,7 +690,11 @@ void launch_as(const LinearGradArgs &a, const Choice &c, hipStream_t st)
     case 1: hipLaunchKernelGGL((k_linear_grad<T, F, 2, 2, 2, 2, 2>), grid, dim3(512), 0, st, a, p); break;
     case 2: hipLaunchKernelGGL((k_linear_grad<T, F, 2, 2, 1, 4, 2>), grid, dim3(512), 0, st, a, p); break;
     case 3: hipLaunchKernelGGL((k_linear_grad<T, F, 1, 1, 2, 2, 2>), grid, dim3(512), 0, st, a, p); break;
-    default: hipLaunchKernelGGL((k_linear_grad_few<T, F>), grid, dim3(kThreads), 0, st, a, p);
+    default:
+        if (a.outs == 1) hipLaunchKernelGGL((k_linear_grad_few<T, F, 1>), grid, dim3(kThreads), 0, st, a, p);
+        else if (a.outs == 2) hipLaunchKernelGGL((k_linear_grad_few<T, F, 2>), grid, dim3(kThreads), 0, st, a, p);
+        else if (a.outs <= 4) hipLaunchKernelGGL((k_linear_grad_few<T, F, 4>), grid, dim3(kThreads), 0, st, a, p);
+        else hipLaunchKernelGGL((k_linear_grad_few<T, F, 8>), grid, dim3(kThreads), 0, st, a, p);
     }
 }
 

@@ -85,7 +85,7 @@ def test_gradients(rows, cols, outs, dtype, fmt, group):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("rows,cols,outs", [(4099, 2047, 1531), (1000, 520, 776), (2500, 64, 2056), (3000, 1100, 70), (1537, 1025, 263),
-                                            (300, 4000, 3), (2000, 9, 520)])
+                                            (300, 4000, 3), (2000, 9, 520), (70000, 8, 2), (3001, 257, 7), (5000, 1, 1), (2000, 100, 4)])
 @pytest.mark.parametrize("dtype", list(TERMS))
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 def test_larger_products(rows, cols, outs, dtype, fmt):
