@@ -142,6 +142,25 @@ def test_strided_unaligned_and_contained(dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", list(TERMS))
+@pytest.mark.parametrize("rows,outs", [(1, 1), (9000, 30), (40000, 3), (70, 1000)])
+def test_bias_alone(dtype, rows, outs):
+    """No columns: the bias gradient only, within rows * 2^-24 of the sum of magnitudes and a rounding to its type; added to what is
+    there when asked."""
+    dy = torch.randn(rows, outs, generator=torch.Generator().manual_seed(rows)).to(dtype).cuda()
+    ck = ops.byte_store(torch.empty(rows, 0, dtype=dtype, device="cuda"))
+    start = torch.randn(outs, generator=torch.Generator().manual_seed(2)).cuda()
+    want = dy.double().cpu().sum(0)
+    tol = rows * 2.0 ** -24 * dy.double().cpu().abs().sum(0) + 1e-37
+    db = ops.byte_linear_grad(dy, ck, bias=True)[1]
+    assert bool(((db.double().cpu() - want).abs() <= tol + ref.HALF_STEP[dtype] * (want.abs() + tol) + 2.0 ** -25).all())
+    held = start.clone()
+    ops.byte_linear_grad(dy, ck, out=torch.empty(outs, 0, device="cuda"), out_bias=held, accumulate=True)
+    both = want + start.double().cpu()
+    assert bool(((held.double().cpu() - both).abs() <= tol + 2.0 ** -23 * (both.abs() + tol)).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TERMS))
 def test_leading_dimensions_and_no_rows(dtype):
     x = torch.randn(3, 5, 40, generator=torch.Generator().manual_seed(3)).to(dtype).cuda()
     dy = torch.randn(3, 5, 24, generator=torch.Generator().manual_seed(4)).to(dtype).cuda()
