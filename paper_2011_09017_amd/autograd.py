@@ -21,6 +21,7 @@ captured into a graph; as with any layer of torch, no eager graph of the same pa
 from __future__ import annotations
 
 import math
+import re
 import weakref
 from dataclasses import dataclass
 from typing import Callable, Iterable, Optional, Union
@@ -177,6 +178,22 @@ class ActivationCompressor:
         return {"top": top, "peak": peak, "held": held, "status": st}
 
 
+# A parameter reaches an operation as it is, as a view of it, or as a copy of either in another type or order.
+_FORMS_OF_A_PARAMETER = re.compile(r"(ToCopy|Clone|T|Transpose|Permute|View|UnsafeView|ReshapeAlias|Select|Slice|Split|SplitWithSizes|Unbind|"
+                                   r"Expand|Squeeze|Unsqueeze|Alias|AsStrided)Backward\d*")
+
+
+def _storage(t: torch.Tensor) -> int:
+    return t.untyped_storage().data_ptr()
+
+
+def _in_autocast() -> bool:
+    # torch.is_autocast_enabled says no inside the operation whose arguments autocast has cast, which is where hooks run
+    depth = torch.autocast_increment_nesting()
+    torch.autocast_decrement_nesting()
+    return depth > 1
+
+
 @dataclass
 class _HeldBytes:
     """What autograd holds instead of a tensor: its checkpoint in the order of its memory, and that order."""
@@ -189,33 +206,58 @@ class ByteCheckpoints:
     whatever the order of its dimensions in memory (channels last included; groups run along the dimension that is
     dense).  A graph can be walked backward as often as autograd allows: checkpoints are only read.
 
-    fmt, group: see operators.byte_store.  min_numel: smaller tensors are saved as they are, and so are parameters,
-    tensors named to skip_parameters, tensors with gaps and those whose rows are too short for eight bits to save anything (a
-    row of codes takes a multiple of 16 bytes).  A value is off by at most 1/127 of the largest in its group
-    ("int8") or 1/16 of itself ("e4m3"): what is not an activation (indices kept as floats, running sums) does not
-    belong under these hooks.
+    fmt, group: see operators.byte_store.  min_numel: smaller tensors are saved as they are, and so are parameters
+    (torch.nn.Parameter, frozen ones too), tensors named to skip_parameters, views of either and copies of them in another type or
+    order (autocast's among them), tensors with gaps and those whose rows are too short for eight bits to save anything (a
+    row of codes takes a multiple of 16 bytes).  Inside an autocast region tensors of its type without a gradient history are saved as
+    they are too: a cast of a frozen weight looks like that.  Weights that are computed in another way (the sum of a weight
+    and its low-rank change, a frozen one cast by the program) look like activations and have to be named.
+
+    A value is off by at most 1/127 of the largest in its group ("int8") or 1/16 of itself ("e4m3"): what is not an activation
+    (indices kept as floats, running sums, statistics that a layer keeps for its backward pass) does not belong under these hooks.
     """
 
     def __init__(self, fmt: str = "int8", group: int = 64, min_numel: int = 1 << 14):
         operators._byte_shape(0, 0, fmt, group)                       # refuses what byte_store would refuse later
         self.fmt, self.group, self.min_numel = fmt, int(group), int(min_numel)
-        self._skip = set()
+        self._named = []                        # weak references: an address means a tensor as long as that lives
+        self._skip = set()                      # their storages
         self.stats = {"packed": 0, "raw_bytes": 0, "held_bytes": 0, "passed_through": 0}
 
     def skip_parameters(self, params: Iterable[torch.Tensor]) -> None:
-        for p in params:
-            self._skip.add(p.data_ptr())
+        self._named += [weakref.ref(p) for p in params]
+        self._find_named()
+
+    def _find_named(self) -> None:
+        alive = [(ref, ref()) for ref in self._named]
+        self._named = [ref for ref, t in alive if t is not None]
+        self._skip = {_storage(t) for _, t in alive if t is not None}
+
+    def _is_weight(self, t: torch.Tensor) -> bool:
+        def known(v):
+            return isinstance(v, torch.nn.Parameter) or _storage(v) in self._skip
+        base = t if t._base is None else t._base
+        if known(base):
+            return True
+        node = base.grad_fn
+        while node is not None and _FORMS_OF_A_PARAMETER.fullmatch(node.name()):
+            node = node.next_functions[0][0]
+        if hasattr(node, "variable"):                                 # a leaf: the tensor that accumulates a gradient
+            return known(node.variable)
+        return not t.requires_grad and t.dtype == torch.get_autocast_dtype(t.device.type) and _in_autocast()
 
     def _held_bytes(self, t: torch.Tensor, order: tuple) -> int:
         cols = t.shape[order[-1]]
         return operators._byte_shape(t.numel() // cols, cols, self.fmt, self.group)[1]
 
     def pack(self, t: torch.Tensor):
+        if (not t.is_cuda or t.layout != torch.strided or t.dtype not in operators._TYPES or t.dim() < 1
+                or t.numel() < max(1, self.min_numel) or self._is_weight(t)):
+            self.stats["passed_through"] += 1
+            return t
         # dimensions of one element last in the order of memory would make rows of one value: they come first
         order = tuple(sorted(range(t.dim()), key=lambda d: (t.shape[d] != 1, -t.stride(d), d)))
-        if (not t.is_cuda or t.dtype not in operators._TYPES or t.dim() < 1 or t.numel() < max(1, self.min_numel)
-                or isinstance(t, torch.nn.Parameter) or t.data_ptr() in self._skip or not t.permute(order).is_contiguous()
-                or self._held_bytes(t, order) >= t.numel() * t.element_size()):
+        if not t.permute(order).is_contiguous() or self._held_bytes(t, order) >= t.numel() * t.element_size():
             self.stats["passed_through"] += 1
             return t
         ck = operators.byte_store(t.detach().permute(order), self.fmt, self.group)
@@ -234,6 +276,7 @@ class ByteCheckpoints:
 
     def hooks(self):
         """Context manager for one forward pass: ``with held.hooks(): loss = model(x)``."""
+        self._find_named()
         return torch.autograd.graph.saved_tensors_hooks(self.pack, self.unpack)
 
 
@@ -303,26 +346,31 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
     return _Linear.apply(x, weight, bias, fmt, group)
 
 
+def _norm_parameters(*params):
+    """gamma and beta as the operators take them."""
+    return tuple(None if p is None else p.float().contiguous() for p in params)
+
+
 class _GroupNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, groups, eps, act, fmt, group):
         x = x.contiguous()
-        w, b = (None if p is None else p.float().contiguous() for p in (weight, bias))
+        w, b = _norm_parameters(weight, bias)
         y, stats, held = operators.group_norm(x, groups, w, b, eps, act, save=fmt, group=group)
         ctx.groups, ctx.act = groups, act
-        ctx.kinds = tuple(None if p is None else p.dtype for p in (weight, bias))
-        _keep(ctx, held, w, b, stats, None if held is not None else x)
+        _keep(ctx, held, weight, bias, stats, None if held is not None else x)    # the parameters as they are: hooks know them
         return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        held, w, b, stats, x = _kept(ctx)
+        held, weight, bias, stats, x = _kept(ctx)
+        w, b = _norm_parameters(weight, bias)
         params = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
         dx, dw, db = operators.group_norm_grad(dy.contiguous(), held if x is None else x, stats, ctx.groups, w, b, ctx.act,
                                                params=params)
-        dw = dw.to(ctx.kinds[0]) if params and ctx.needs_input_grad[1] else None
-        db = db.to(ctx.kinds[1]) if params and ctx.needs_input_grad[2] else None
+        dw = dw.to(weight.dtype) if params and ctx.needs_input_grad[1] else None
+        db = db.to(bias.dtype) if params and ctx.needs_input_grad[2] else None
         return dx if ctx.needs_input_grad[0] else None, dw, db, None, None, None, None, None
 
 
