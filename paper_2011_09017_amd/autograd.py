@@ -27,6 +27,7 @@ from dataclasses import dataclass
 from typing import Callable, Iterable, Optional, Union
 
 import torch
+from torch.multiprocessing.reductions import StorageWeakRef
 
 from . import binding, operators
 
@@ -204,7 +205,8 @@ class _HeldBytes:
 class ByteCheckpoints:
     """saved_tensors_hooks that hold every saved fp32, fp16 or bf16 tensor as a byte checkpoint, whatever its shape and
     whatever the order of its dimensions in memory (channels last included; groups run along the dimension that is
-    dense).  A graph can be walked backward as often as autograd allows: checkpoints are only read.
+    dense).  A graph can be walked backward as often as autograd allows: checkpoints are only read.  What several
+    operations of a forward pass save (the input of three projections) is held once, as autograd itself has it.
 
     fmt, group: see operators.byte_store.  min_numel: smaller tensors are saved as they are, and so are parameters
     (torch.nn.Parameter, frozen ones too), tensors named to skip_parameters, views of either and copies of them in another type or
@@ -222,7 +224,8 @@ class ByteCheckpoints:
         self.fmt, self.group, self.min_numel = fmt, int(group), int(min_numel)
         self._named = []                        # weak references: an address means a tensor as long as that lives
         self._skip = set()                      # their storages
-        self.stats = {"packed": 0, "raw_bytes": 0, "held_bytes": 0, "passed_through": 0}
+        self._by_memory = {}                    # what memory held -> (weak ref of its storage, of its checkpoint's bytes), current forward pass
+        self.stats = {"packed": 0, "shared": 0, "raw_bytes": 0, "held_bytes": 0, "passed_through": 0}
 
     def skip_parameters(self, params: Iterable[torch.Tensor]) -> None:
         self._named += [weakref.ref(p) for p in params]
@@ -260,7 +263,20 @@ class ByteCheckpoints:
         if not t.permute(order).is_contiguous() or self._held_bytes(t, order) >= t.numel() * t.element_size():
             self.stats["passed_through"] += 1
             return t
-        ck = operators.byte_store(t.detach().permute(order), self.fmt, self.group)
+        # Saved before and not changed since: the checkpoint of the same dense rows, whatever their shape (a layer of matrices saves a
+        # view of its own).  The weak references tell live memory from recycled addresses and bytes in use from freed
+        # ones; another stream has nothing to wait for the first one's store with, and a graph's replays do not repeat a store that was not captured.
+        rows = t.detach().permute(order)
+        storage = t.untyped_storage()
+        key = (storage._cdata, t.storage_offset(), t.numel(), rows.shape[-1], t.dtype, t._version, operators._stream(t.device),
+               torch.cuda.is_current_stream_capturing())
+        hit = self._by_memory.get(key)
+        buf = None if hit is None or hit[0].expired() else hit[1]()
+        if buf is not None:
+            self.stats["shared"] += 1
+            return _HeldBytes(operators.ByteCheckpoint(buf, tuple(rows.shape), t.dtype, self.fmt, self.group), order)
+        ck = operators.byte_store(rows, self.fmt, self.group)
+        self._by_memory[key] = (StorageWeakRef(storage), weakref.ref(ck.buf))
         self.stats["packed"] += 1
         self.stats["raw_bytes"] += t.numel() * t.element_size()
         self.stats["held_bytes"] += ck.nbytes
@@ -277,6 +293,7 @@ class ByteCheckpoints:
     def hooks(self):
         """Context manager for one forward pass: ``with held.hooks(): loss = model(x)``."""
         self._find_named()
+        self._by_memory = {}
         return torch.autograd.graph.saved_tensors_hooks(self.pack, self.unpack)
 
 

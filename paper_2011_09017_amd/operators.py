@@ -10,8 +10,8 @@ activation as a *byte checkpoint* and compute a layer's backward pass from it:
 
 Formats, formulas, limits and error bounds are those of include/cmpz.h.  The functions run on the current stream of
 their tensors' GPU (which need not be the current GPU), wait for nothing, and may be captured into a graph; outputs and
-workspaces that the caller does not pass come from torch's allocator.  They know nothing of autograd: gradients flow
-through :mod:`.autograd`'s functions.  Wrong arguments raise ValueError before anything is launched, what the library
+workspaces that the caller does not pass come from torch's allocator.  They know nothing of autograd but that what a caller
+passes to be written counts as changed: gradients flow through :mod:`.autograd`'s functions.  Wrong arguments raise ValueError before anything is launched, what the library
 refuses raises :class:`.binding.CmpError`.
 """
 from __future__ import annotations
@@ -52,9 +52,13 @@ def _stream(dev: torch.device) -> int:
     return torch._C._cuda_getCurrentRawStream(dev.index)          # the current stream's handle, without a Stream object
 
 
-def _call(rc: int, where: str) -> None:
+def _call(rc: int, where: str, *written) -> None:
+    """`written`: tensors of the caller's that the call has changed, None among them."""
     if rc != binding.CMP_OK:
         raise binding.CmpError(rc, where)
+    for t in written:
+        if t is not None:
+            torch.autograd.graph.increment_version(t)
 
 
 def _rows_of(t: torch.Tensor):
@@ -135,11 +139,12 @@ def byte_store(x: torch.Tensor, fmt: str = "int8", group: int = 64, out: Optiona
     rows, ld = _matrix(x, "byte_store")
     shape, nbytes = _byte_shape(rows, x.shape[-1], fmt, group)
     dev = _on_gpu(x, out)
+    given = out
     if out is None:
         out = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     _refuse(out.dtype != torch.uint8 or not out.is_contiguous(), "byte_store: out has to be a contiguous uint8 tensor")
     _call(binding.cmp_byte_store(dev.index, shape, x.data_ptr(), kind, ld, out.data_ptr(), out.numel(),
-                                 _stream(dev)), "cmp_byte_store")
+                                 _stream(dev)), "cmp_byte_store", given)
     return ByteCheckpoint(out, tuple(x.shape), x.dtype, fmt, group)
 
 
@@ -147,6 +152,7 @@ def byte_load(ck: ByteCheckpoint, dtype: Optional[torch.dtype] = None, out: Opti
     """Restores a checkpoint, in the type it was stored from unless `dtype` or `out` says otherwise."""
     shape = _held(ck)
     dev = _on_gpu(ck.buf, out)
+    given = out
     if out is None:
         out = torch.empty(ck.shape, dtype=dtype or ck.dtype, device=dev)
     _refuse(tuple(out.shape) != tuple(ck.shape), "byte_load: out has another shape than the checkpoint")
@@ -154,7 +160,7 @@ def byte_load(ck: ByteCheckpoint, dtype: Optional[torch.dtype] = None, out: Opti
     kind = _type_of(out)
     rows, ld = _matrix(out, "byte_load")
     _call(binding.cmp_byte_load(dev.index, shape, ck.buf.data_ptr(), ck.buf.numel(), out.data_ptr(), kind, ld,
-                                _stream(dev)), "cmp_byte_load")
+                                _stream(dev)), "cmp_byte_load", given)
     return out
 
 
@@ -171,6 +177,7 @@ def byte_linear_grad(dy: torch.Tensor, ck: ByteCheckpoint, bias: bool = False, d
     _refuse(accumulate and out is None, "byte_linear_grad: accumulate needs out")
     _refuse(accumulate and bias and out_bias is None, "byte_linear_grad: accumulate with a bias needs out_bias")
     _refuse(out is not None and dtype is not None and out.dtype != dtype, "byte_linear_grad: out has another type than dtype")
+    given = out, out_bias
     dtype = out.dtype if out is not None else dtype or dy.dtype
     _refuse(dtype not in (dy.dtype, torch.float32), "byte_linear_grad: results are in dy's type or float32")
     if out is None:
@@ -185,7 +192,7 @@ def byte_linear_grad(dy: torch.Tensor, ck: ByteCheckpoint, bias: bool = False, d
     _call(binding.cmp_byte_linear_grad(dev.index, shape, ck.buf.data_ptr(), ck.buf.numel(), dy.data_ptr(), kind, outs, ld,
                                        out.data_ptr(), None if out_bias is None else out_bias.data_ptr(), _TYPES[dtype],
                                        accumulate, None if work is None else work.data_ptr(), need,
-                                       _stream(dev)), "cmp_byte_linear_grad")
+                                       _stream(dev)), "cmp_byte_linear_grad", *given)
     return out, out_bias
 
 

@@ -163,3 +163,108 @@ def test_the_layers_own_parameters_stay_as_they_are(dtype):
         got.append(torch.autograd.grad(y, (x, gamma, beta, w), dy))
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+def _input(dtype=torch.bfloat16, shape=(4, 32, 256), seed=5):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(DEV, dtype).requires_grad_()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(128, 256), (4, 32, 256)])
+def test_what_several_layers_save_is_held_once(shape):
+    """Three projections of one activation: one checkpoint, the gradients of three, and the memory back behind the backward
+    pass although the hooks live on."""
+    torch.manual_seed(6)
+    layers = [torch.nn.Linear(256, 128).to(DEV, torch.bfloat16) for _ in range(3)]
+    x = _input(shape=shape)
+    held = ByteCheckpoints("int8", 64, min_numel=1 << 10)
+    dy = torch.randn(*shape[:-1], 128, generator=torch.Generator().manual_seed(7)).to(DEV, torch.bfloat16)
+    with held.hooks():
+        h = x * 2                                                 # (saves nothing)
+        ys = [layer(h) for layer in layers]
+    one = 128 * (256 + 256 // 64)
+    assert held.stats["packed"] == 1 and held.stats["shared"] == 2 and held.stats["held_bytes"] == one
+    assert held.stats["raw_bytes"] == 2 * x.numel()
+    got = torch.autograd.grad([y for y in ys], [layer.weight for layer in layers], [dy] * 3, retain_graph=True)
+    again = torch.autograd.grad([y for y in ys], [layer.weight for layer in layers], [dy] * 3)
+    x2 = ops.byte_load(ops.byte_store(h.detach().view(-1, 256), "int8", 64))
+    for layer, g, a in zip(layers, got, again):
+        want = torch.autograd.grad(layer(x2), layer.weight, dy.view(-1, 128))[0]
+        assert torch.equal(g, want) and torch.equal(a, want)
+
+
+@pytest.mark.gpu
+def test_shared_bytes_are_freed_with_their_last_user():
+    x = _input(shape=(512, 1024))
+    w = [torch.nn.Parameter(torch.randn(8, 1024, device=DEV).bfloat16()) for _ in range(2)]
+    held = ByteCheckpoints(min_numel=1 << 12)
+
+    def step():
+        with held.hooks():
+            h = x * 2
+            return sum(F.linear(h, v) for v in w).float().square().sum()
+    step().backward()
+    before = torch.cuda.memory_allocated()
+    loss = step()
+    assert torch.cuda.memory_allocated() >= before + 512 * 1024
+    loss.backward()
+    torch.cuda.synchronize()
+    assert torch.cuda.memory_allocated() < before + 512 * 1024
+    assert held.stats["packed"] == 4 and held.stats["shared"] == 2   # two steps: h and the square's 512 x 8 values; h's second user
+
+
+@pytest.mark.gpu
+def test_what_changed_or_lies_elsewhere_is_not_shared():
+    """The same memory after a change in place, another part of it, another last dimension, another type of its bytes, the
+    same addresses after the tensor is gone, and another stream: each has a checkpoint of its own."""
+    held = ByteCheckpoints("e4m3", 32, min_numel=1)
+    values = lambda t: ops.byte_load(ops.byte_store(t.contiguous(), "e4m3", 32))  # noqa: E731
+    with held.hooks():
+        x = _input(shape=(64, 256)).detach()
+        first = held.pack(x)
+        want = values(x)
+        assert torch.equal(held.unpack(held.pack(x.view(2, 32, 256))).view(64, 256), want) and held.stats["shared"] == 1
+        assert torch.equal(held.unpack(held.pack(x.unsqueeze(1)))[:, 0], want) and held.stats["shared"] == 2
+        turned = x.t()                                            # the same rows in memory, seen from the other side
+        assert torch.equal(held.unpack(held.pack(turned)), want.t()) and held.stats["shared"] == 3
+        for v in (x[:32], x[32:], x.view(32, 512), x.view(torch.float16)):
+            assert torch.equal(held.unpack(held.pack(v)).nan_to_num(), values(v).nan_to_num())
+        assert held.stats["shared"] == 3
+        x.mul_(3)
+        assert torch.equal(held.unpack(held.pack(x)), values(x)) and held.stats["shared"] == 3
+        assert torch.equal(held.unpack(first), want)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            other = held.pack(x)
+        torch.cuda.synchronize()
+        assert held.stats["shared"] == 3 and torch.equal(held.unpack(other), values(x))
+        kept = []
+        for k in range(4):                                        # one address after the other
+            t = torch.full((64, 256), float(k + 1), device=DEV, dtype=torch.bfloat16)
+            kept.append(held.pack(t))
+            del t
+        assert held.stats["shared"] == 3
+        for k, h in enumerate(kept):
+            assert bool((held.unpack(h) == k + 1).all())
+        n = held.stats["packed"]
+        x2 = _input(shape=(64, 256)).detach()
+        held.pack(x2)                                             # dropped at once: nothing to share
+        held.pack(x2)
+        assert held.stats["packed"] == n + 2
+
+
+@pytest.mark.gpu
+def test_a_buffer_written_by_an_operator_counts_as_changed():
+    """A caller's buffer that an operator fills between two layers: each layer's checkpoint is of what it saw."""
+    held = ByteCheckpoints("int8", 32, min_numel=1)
+    a, b = (ops.byte_store(_input(shape=(64, 256), seed=s).detach()) for s in (8, 9))
+    buf = torch.empty(64, 256, device=DEV, dtype=torch.bfloat16)
+    with held.hooks():
+        kept = [held.pack(ops.byte_load(ck, out=buf)) for ck in (a, b)]
+    assert held.stats["shared"] == 0 and not torch.equal(held.unpack(kept[0]), held.unpack(kept[1]))
+    outs = [torch.zeros(a.nbytes, dtype=torch.uint8, device=DEV), torch.zeros(8, 256, device=DEV), torch.zeros(8, device=DEV)]
+    dy, before = torch.ones(64, 8, device=DEV), [t._version for t in outs]
+    ops.byte_store(buf, "int8", 64, out=outs[0])
+    ops.byte_linear_grad(dy, a, out=outs[1], out_bias=outs[2])
+    assert [t._version for t in outs] == [v + 1 for v in before]
