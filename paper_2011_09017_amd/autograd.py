@@ -325,9 +325,12 @@ def _product(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor]
 class _Linear(torch.autograd.Function):
     @staticmethod
     @torch.amp.custom_fwd(device_type="cuda")
-    def forward(ctx, x, weight, bias, fmt, group):
+    def forward(ctx, x, weight, bias, fmt, group, held):
         rows = _dense_rows(x)
-        held = operators.byte_store(rows, fmt, group) if ctx.needs_input_grad[1] else None
+        if not ctx.needs_input_grad[1]:
+            held = None
+        elif held is None:
+            held = operators.byte_store(rows, fmt, group)
         _keep(ctx, held, weight if ctx.needs_input_grad[0] else None)
         ctx.kinds = (x.dtype, weight.dtype, None if bias is None else bias.dtype)
         return _product(rows, weight, bias)
@@ -350,17 +353,24 @@ class _Linear(torch.autograd.Function):
             db = _as_matrix(dy).sum(0, dtype=torch.float32)
         if db is not None:
             db = db.to(ctx.kinds[2])
-        return dx, dw, db, None, None
+        return dx, dw, db, None, None, None
 
 
-def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, fmt: str = "int8", group: int = 64):
+def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, fmt: str = "int8", group: int = 64,
+           held: Optional[operators.ByteCheckpoint] = None):
     """torch.nn.functional.linear whose input is held as a byte checkpoint; the weight's (and bias's) gradient is computed from
-    the eight-bit form by operators.byte_linear_grad.  x: [..., cols] in float32, float16 or bfloat16 on a GPU.  Without a
-    backward pass to come (torch.no_grad) nothing is stored."""
+    the eight-bit form by operators.byte_linear_grad.  x: [..., cols] in float32, float16 or bfloat16 on a GPU.  held: x's
+    checkpoint where there is one already (operators.byte_store(x), for several layers of one input): it is read in place of a new
+    one, and fmt and group are its own.  Without a backward pass to come (torch.no_grad) nothing is stored."""
     operators._byte_shape(0, 0, fmt, group)                           # refuses a bad format in either case
+    if held is not None:
+        operators._refuse(not isinstance(held, operators.ByteCheckpoint) or tuple(held.shape) != tuple(x.shape),
+                          "linear: held has to be the checkpoint of x")
+        operators._refuse(held.nbytes < binding.cmp_byte_bytes(operators._held(held)), "linear: held is too short for its shape")
+        operators._refuse(held.buf.device != x.device, "linear: held is on another GPU than x")
     if not torch.is_grad_enabled():
         return _product(x, weight, bias)
-    return _Linear.apply(x, weight, bias, fmt, group)
+    return _Linear.apply(x, weight, bias, fmt, group, held)
 
 
 def _norm_parameters(*params):

@@ -268,3 +268,38 @@ def test_a_buffer_written_by_an_operator_counts_as_changed():
     ops.byte_store(buf, "int8", 64, out=outs[0])
     ops.byte_linear_grad(dy, a, out=outs[1], out_bias=outs[2])
     assert [t._version for t in outs] == [v + 1 for v in before]
+
+
+def test_linear_refuses_another_tensors_checkpoint():
+    from paper_2011_09017_amd.autograd import linear
+    x, w = torch.randn(3, 5, 32), torch.randn(7, 32, requires_grad=True)
+    buf = torch.empty(15 * 33 + 1, dtype=torch.uint8)
+    good = ops.ByteCheckpoint(buf, (3, 5, 32), torch.float32, "int8", 32)
+    with torch.no_grad():
+        assert torch.equal(linear(x, w, held=good), F.linear(x, w))
+    for bad in (good._replace(shape=(15, 32)), good._replace(fmt="int4"), good._replace(group=48), good._replace(buf=buf.int()),
+                good._replace(buf=buf[::2]), good._replace(buf=buf[:400]), buf, good._replace(buf=buf.to("meta"))):
+        for grad in (True, False):
+            with torch.set_grad_enabled(grad), pytest.raises(ValueError):
+                linear(x, w, held=bad)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group", [("int8", 64), ("e4m3", 128)])
+def test_layers_of_one_input_share_a_checkpoint(fmt, group, monkeypatch):
+    """Three projections of one activation from one checkpoint: what each gives with its own, and one checkpoint's memory."""
+    from paper_2011_09017_amd.autograd import linear
+    gen = torch.Generator().manual_seed(10)
+    ws = [torch.nn.Parameter(torch.randn(n, 256, generator=gen).to(DEV, torch.bfloat16)) for n in (128, 64, 64)]
+    bs = [torch.nn.Parameter(torch.randn(len(w), generator=gen).to(DEV, torch.bfloat16)) for w in ws]
+    x = _input()
+    dys = [torch.randn(4, 32, len(w), generator=gen).to(DEV, torch.bfloat16) for w in ws]
+    want = torch.autograd.grad([linear(x, w, b, fmt, group) for w, b in zip(ws, bs)], [x, *ws, *bs], dys)
+    stores = []
+    real = ops.byte_store
+    monkeypatch.setattr(ops, "byte_store", lambda *a, **kw: (stores.append(1), real(*a, **kw))[1])
+    held = ops.byte_store(x.detach(), fmt, group)
+    ys = [linear(x, w, b, held=held) for w, b in zip(ws, bs)]
+    for a, b in zip(torch.autograd.grad(ys, [x, *ws, *bs], dys), want):
+        assert torch.equal(a, b)
+    assert len(stores) == 1
