@@ -361,7 +361,8 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
     """torch.nn.functional.linear whose input is held as a byte checkpoint; the weight's (and bias's) gradient is computed from
     the eight-bit form by operators.byte_linear_grad.  x: [..., cols] in float32, float16 or bfloat16 on a GPU.  held: x's
     checkpoint where there is one already (operators.byte_store(x), for several layers of one input): it is read in place of a new
-    one, and fmt and group are its own.  Without a backward pass to come (torch.no_grad) nothing is stored."""
+    one, and fmt and group are its own.  Without a backward pass to come (torch.no_grad, or a weight that needs
+    no gradient) nothing is stored."""
     operators._byte_shape(0, 0, fmt, group)                           # refuses a bad format in either case
     if held is not None:
         operators._refuse(not isinstance(held, operators.ByteCheckpoint) or tuple(held.shape) != tuple(x.shape),
@@ -383,7 +384,8 @@ class _GroupNorm(torch.autograd.Function):
     def forward(ctx, x, weight, bias, groups, eps, act, fmt, group):
         x = x.contiguous()
         w, b = _norm_parameters(weight, bias)
-        y, stats, held = operators.group_norm(x, groups, w, b, eps, act, save=fmt, group=group)
+        save = fmt if any(ctx.needs_input_grad) else None
+        y, stats, held = operators.group_norm(x, groups, w, b, eps, act, save=save, group=group)
         ctx.groups, ctx.act = groups, act
         _keep(ctx, held, weight, bias, stats, None if held is not None else x)    # the parameters as they are: hooks know them
         return y
@@ -405,7 +407,7 @@ def group_norm(x: torch.Tensor, groups: int, weight: Optional[torch.Tensor] = No
                eps: float = 1e-5, act: str = "none", fmt: Optional[str] = "int8", group: int = 64):
     """Group norm and activation of x[batch, ..., channels] (channels last: permute an NCHW tensor to NHWC first, which costs
     nothing for one in torch's channels_last format).  Its input is held as a byte checkpoint written in the same pass;
-    fmt=None holds x itself.  Without a backward pass to come (torch.no_grad) nothing is stored."""
+    fmt=None holds x itself.  Without a backward pass to come (torch.no_grad, or nothing that needs a gradient) nothing is stored."""
     if fmt is not None:
         operators._byte_shape(0, 0, fmt, group)                       # refuses a bad format in either case
     return _GroupNorm.apply(x, weight, bias, groups, eps, act, fmt if torch.is_grad_enabled() else None, group)

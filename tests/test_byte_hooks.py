@@ -303,3 +303,21 @@ def test_layers_of_one_input_share_a_checkpoint(fmt, group, monkeypatch):
     for a, b in zip(torch.autograd.grad(ys, [x, *ws, *bs], dys), want):
         assert torch.equal(a, b)
     assert len(stores) == 1
+
+
+@pytest.mark.parametrize("learns", range(4))
+def test_a_norm_that_nothing_learns_from_stores_nothing(learns, monkeypatch):
+    """With gradients enabled a checkpoint is written if one of input, weight and bias needs one (0: none does)."""
+    from paper_2011_09017_amd.autograd import group_norm
+    asked = []
+
+    def norm(x, groups, w, b, eps, act, save=None, group=64):
+        asked.append(save)
+        ck = None if save is None else ops.ByteCheckpoint(torch.empty(0, dtype=torch.uint8), tuple(x.shape), x.dtype, save, group)
+        return torch.empty_like(x), torch.empty(x.shape[0], groups, 2, dtype=torch.float64), ck
+    monkeypatch.setattr(ops, "group_norm", norm)
+    ts = [torch.randn(s) for s in ((2, 9, 32), (32,), (32,))]
+    if learns:
+        ts[learns - 1].requires_grad_()
+    y = group_norm(ts[0], 4, ts[1], ts[2], fmt="e4m3")
+    assert asked == ["e4m3" if learns else None] and y.requires_grad == bool(learns)
