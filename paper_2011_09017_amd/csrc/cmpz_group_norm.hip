@@ -203,13 +203,18 @@ __device__ __forceinline__ double group_total(uint32_t g, uint32_t per, uint32_t
 
 // ---- forward ------------------------------------------------------------------------------------------
 
-// Sums and sums of squares in fp64, which the vector units add at the rate of fp32: no cancellation however far
-// the mean lies from zero, and no second pass over the data for the variance.
-__device__ __forceinline__ void add_moments(f32x8 v, double (&s1)[8], double (&s2)[8])
+// Sums and sums of squares in fp64, which the vector units add at the rate of fp32, and no second pass over the data for the
+// variance E[x^2] - E[x]^2 while that is at least kUnsure of E[x^2]: with 2^-53 to a rounding it is right to 2^-26 then.  Where
+// it is less (a mean some 256 deviations from zero), the workgroup adds up its values a second time, less a value near
+// their mean: they are in registers or caches (256 x 49 x 512 fp32: 13.8 us, so 18.9; 64 x 3136 x 256: 127 and 149).  All
+// values less the first of their group, at once, would cost everyone 8 to 10 % (256 x 49 x 512 fp32 with codes: 18.6 us and 19.9).
+constexpr double kUnsure = 0x1p-16;
+template <bool ABOUT>
+__device__ __forceinline__ void add_moments(f32x8 v, const float (&at)[8], double (&s1)[8], double (&s2)[8])
 {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const double d = (double)v[k];
+        const double d = ABOUT ? (double)v[k] - (double)at[k] : (double)v[k];
         s1[k] += d;
         s2[k] = __builtin_fma(d, d, s2[k]);
     }
@@ -258,22 +263,34 @@ __device__ __forceinline__ void join_moments(double *s, double (&s1)[8], double 
     }
 }
 
-struct Moments { double mean, rstd; };
-__device__ __forceinline__ Moments moments_of(const NormArgs &a, const Plan &p, double s1, double s2)
+// From the sums about `at`.  unsure: kUnsure.
+struct Moments { double mean, rstd; bool unsure; };
+__device__ __forceinline__ Moments moments_of(const NormArgs &a, const Plan &p, double at, double s1, double s2)
 {
-    const double mean = s1 * p.share;
-    double var = s2 * p.share - mean * mean;
+    const double off = s1 * p.share, square = s2 * p.share;
+    double var = square - off * off;
     if (var < 0.0) var = 0.0;
     var += a.eps;
+    const bool unsure = var < kUnsure * square;
     // an approximation of 26 bits and two steps of Newton's method: a division and a square root take four times as long
     double r = __builtin_amdgcn_rsq(var);
     r = r * __builtin_fma(-0.5 * var * r, r, 1.5);
     r = r * __builtin_fma(-0.5 * var * r, r, 1.5);
-    return {mean, r};
+    // a mean that is an fp32 number but for the roundings of its division is one: that of equal values is their value
+    double mean = at + off;
+    const double near = (double)(float)mean;
+    if (fabs(mean - near) <= 0x1p-48 * fabs(mean)) mean = near;
+    return {mean, r, unsure};
 }
 
-// u = (x - mean) * mul + add of a thread's channels (a group of equal values gives exactly `add`).  m: mean and
-// 1 / deviation of the groups, the first that of channel `first`.
+// u = (x - mean) * mul + add of a thread's channels (a group of equal values gives exactly beta): what the mean loses in
+// its rounding to fp32 is in `add`.
+struct __align__(16) Group { float mean, lost; double rstd; };            // mean + lost: the mean
+__device__ __forceinline__ Group group_of(double mean, double rstd)
+{
+    const float near = (float)mean;
+    return {near, (float)(mean - (double)near), rstd};
+}
 struct Line { float mean[8], mul[8], add[8]; };
 __device__ __forceinline__ Line parameters_of(const NormArgs &a, const Place &q)
 {
@@ -288,14 +305,16 @@ __device__ __forceinline__ Line parameters_of(const NormArgs &a, const Place &q)
     }
     return l;
 }
-__device__ __forceinline__ void apply_moments(Line *l, const Plan &p, const Place &q, const double *m, uint32_t first)
+template <class FN>
+__device__ __forceinline__ void apply_moments(Line *l, const Plan &p, const Place &q, uint32_t first, FN of_group)
 {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         if (k < q.valid) {
-            const uint32_t g = p.div_per.div(q.c + k - first);
-            l->mean[k] = (float)m[2 * g];
-            l->mul[k] = (float)(m[2 * g + 1] * (double)l->mul[k]);
+            const Group m = of_group(p.div_per.div(q.c + k - first));
+            l->mean[k] = m.mean;
+            l->mul[k] = (float)(m.rstd * (double)l->mul[k]);
+            l->add[k] = __builtin_fmaf(-m.lost, l->mul[k], l->add[k]);
         }
     }
 }
@@ -341,12 +360,15 @@ template <uint32_t T, uint32_t F, bool EVEN>
 __global__ __launch_bounds__(kMaxThreads) void k_norm_slab(NormArgs a, Plan p)
 {
     extern __shared__ double s_sum[];
+    __shared__ uint32_t s_unsure;
     typedef typename ElemOf<T>::type E;
     Place q = place(p, blockIdx.x, 0, 0);
     const uint32_t first = q.chunk * p.nv * 8u, end = a.channels - first < p.nv * 8u ? a.channels : first + p.nv * 8u;
     q = place(p, blockIdx.x, first, end);
     const uint64_t row0 = (uint64_t)q.n * a.spatial;
+    if (threadIdx.x == 0) s_unsure = 0;                                   // (barriers lie between this and what sets it)
     f32x8 x[kSlabRows];
+    float at[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     double s1[8], s2[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) s1[k] = s2[k] = 0.0;
@@ -358,21 +380,46 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_slab(NormArgs a, Plan p)
     }
     Line l = parameters_of(a, q);
 #pragma unroll
-    for (uint32_t i = 0; i < kSlabRows; ++i) add_moments(x[i], s1, s2);
+    for (uint32_t i = 0; i < kSlabRows; ++i) add_moments<false>(x[i], at, s1, s2);
     const uint32_t groups = (end - first) / p.per;
-    double *m = s_sum + (p.per < 8u ? 16u : 4u) * blockDim.x;
-    join_moments(s_sum, s1, s2, groups, p, q, first, [&](uint32_t g, double t1, double t2) {
-        const Moments v = moments_of(a, p, t1, t2);
-        m[2 * g] = v.mean;
-        m[2 * g + 1] = v.rstd;
+    Group *m = reinterpret_cast<Group *>(s_sum + (p.per < 8u ? 16u : 4u) * blockDim.x);
+    auto give = [&](uint32_t g, const Moments &v) {
+        m[g] = group_of(v.mean, v.rstd);
         if (a.stats) {
             double *st = a.stats + ((uint64_t)q.n * a.groups + p.div_per.div(first) + g) * 2;
             st[0] = v.mean;
             st[1] = v.rstd;
         }
+    };
+    join_moments(s_sum, s1, s2, groups, p, q, first, [&](uint32_t g, double t1, double t2) {
+        const Moments v = moments_of(a, p, 0.0, t1, t2);
+        if (v.unsure) s_unsure = 1;
+        give(g, v);
     });
     __syncthreads();
-    apply_moments(&l, p, q, m, first);
+    if (s_unsure) {                                                       // (uniform) about the means as they are so far
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            s1[k] = s2[k] = 0.0;
+            if (k < q.valid) at[k] = m[p.div_per.div(q.c + k - first)].mean;
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kSlabRows; ++i) {
+            f32x8 v;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                float f = q.r + i * p.rp < a.spatial ? x[i][k] : at[k];
+                asm volatile("" : "+v"(f));                               // else the fp64 forms of all values are kept from above
+                v[k] = f;
+            }
+            add_moments<true>(v, at, s1, s2);
+        }
+        join_moments(s_sum, s1, s2, groups, p, q, first, [&](uint32_t g, double t1, double t2) {
+            give(g, moments_of(a, p, (double)m[g].mean, t1, t2));
+        });
+        __syncthreads();
+    }
+    apply_moments(&l, p, q, first, [&](uint32_t g) { return m[g]; });
     if (F != kPlain) put_tail(a);
 #pragma unroll
     for (uint32_t i = 0; i < kSlabRows; ++i) {
@@ -382,18 +429,24 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_slab(NormArgs a, Plan p)
     }
 }
 
+// A workgroup's record of a group: the mean of its values, and the sum of the squares of their distances from it.
 template <uint32_t T, bool EVEN>
 __global__ __launch_bounds__(kMaxThreads) void k_norm_sums(NormArgs a, Plan p)
 {
     extern __shared__ double s_sum[];
+    __shared__ uint32_t s_unsure;
     typedef typename ElemOf<T>::type E;
     const Place q = place(p, blockIdx.x, 0, a.channels);
     const uint32_t beg = q.chunk * p.rows_per, end = a.spatial - beg < p.rows_per ? a.spatial : beg + p.rows_per;
+    if (threadIdx.x == 0) s_unsure = 0;                                   // (barriers lie between this and what sets it)
+    const E *row0 = static_cast<const E *>(a.x) + ((uint64_t)q.n * a.spatial + beg) * a.channels;
+    float at[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     double s1[8], s2[8];
+    auto add_up = [&](auto about) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) s1[k] = s2[k] = 0.0;
-    if (q.valid > 0) {
-        const E *x = static_cast<const E *>(a.x) + ((uint64_t)q.n * a.spatial + beg + q.r) * a.channels + q.c;
+        for (int k = 0; k < 8; ++k) s1[k] = s2[k] = 0.0;
+        if (q.valid <= 0) return;
+        const E *x = row0 + (uint64_t)q.r * a.channels + q.c;
         const uint64_t step = (uint64_t)p.rp * a.channels;
         const int n = EVEN ? 8 : q.valid;
         uint32_t left = end - beg > q.r ? (end - beg - q.r + p.rp - 1) / p.rp : 0;      // positions of this thread
@@ -402,15 +455,31 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_sums(NormArgs a, Plan p)
 #pragma unroll
             for (uint32_t i = 0; i < 4; ++i) v[i] = load8<T>(x + i * step, n);
 #pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) add_moments(v[i], s1, s2);
+            for (uint32_t i = 0; i < 4; ++i) add_moments<decltype(about)::value>(v[i], at, s1, s2);
         }
-        for (; left; --left, x += step) add_moments(load8<T>(x, n), s1, s2);
-    }
-    double *part = static_cast<double *>(a.work);
+        for (; left; --left, x += step) add_moments<decltype(about)::value>(load8<T>(x, n), at, s1, s2);
+    };
+    const double count = (double)(end - beg) * (double)p.per, share = 1.0 / count;
+    auto give = [&](uint32_t g, double mean, double squares) {
+        double *o = static_cast<double *>(a.work) + (((uint64_t)q.n * a.groups + g) * p.chunks + q.chunk) * 2;
+        o[0] = mean;
+        o[1] = squares < 0.0 ? 0.0 : squares;
+    };
+    add_up(std::false_type{});
     join_moments(s_sum, s1, s2, a.groups, p, q, 0, [&](uint32_t g, double t1, double t2) {
-        double *o = part + (((uint64_t)q.n * a.groups + g) * p.chunks + q.chunk) * 2;
-        o[0] = t1;
-        o[1] = t2;
+        const double mean = t1 * share, squares = t2 - t1 * mean;
+        if (squares + a.eps * count < kUnsure * t2) s_unsure = 1;
+        give(g, mean, squares);
+    });
+    __syncthreads();
+    if (s_unsure == 0) return;                                            // (uniform) about the groups' first values here
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (k < q.valid) at[k] = (float)row0[p.div_per.div(q.c + k) * p.per];
+    add_up(std::true_type{});
+    join_moments(s_sum, s1, s2, a.groups, p, q, 0, [&](uint32_t g, double t1, double t2) {
+        const double off = t1 * share;
+        give(g, (double)row0[g * p.per] + off, t2 - t1 * off);
     });
 }
 
@@ -425,14 +494,23 @@ __device__ __forceinline__ Totals join_chunks(const double *part, uint64_t sampl
     return {wave_sum(t1), wave_sum(t2)};
 }
 
-// Mean and 1 / deviation of every sample and group, between the two passes.  A launch of its own costs 3 us; with this in
-// the prologue of the second pass's workgroups, each of them reads all of its sample's partial sums (one sample of
-// 65536 x 128: 41.6 us where the three launches take 33.8; 64 samples of 3136 x 256: 72 and 76).
+// Mean and 1 / deviation of every sample and group, between the two passes, from the workgroups' records about the first one's
+// mean.  A launch of its own costs 3 us; with this in the prologue of the second pass's workgroups, each of them reads all of
+// its sample's records: one sample of 65536 x 128 takes 41.6 us so where the three launches take 33.8, but 64 samples of 3136 x
+// 256 take 72 where they take 76.  The launch is taken always; the line between the two has not been drawn.
 __global__ __launch_bounds__(kMaxThreads) void k_norm_join(NormArgs a, Plan p, double *stats)
 {
+    const double full = (double)p.rows_per * (double)p.per, last = (double)(a.spatial - (p.chunks - 1u) * p.rows_per) * (double)p.per;
     for (uint64_t i = blockIdx.x * 16ull + (threadIdx.x >> 6); i < a.batch * a.groups; i += gridDim.x * 16ull) {
-        const Totals t = join_chunks(static_cast<const double *>(a.work), i, p);
-        const Moments v = moments_of(a, p, t.t1, t.t2);
+        const double *at = static_cast<const double *>(a.work) + i * p.chunks * 2, near = at[0];
+        double t1 = 0.0, t2 = 0.0;
+#pragma unroll 4
+        for (uint32_t c = threadIdx.x & 63u; c < p.chunks; c += 64u) {
+            const double off = at[2 * c] - near, sum = (c + 1u < p.chunks ? full : last) * off;
+            t1 += sum;
+            t2 += __builtin_fma(sum, off, at[2 * c + 1]);
+        }
+        const Moments v = moments_of(a, p, near, wave_sum(t1), wave_sum(t2));
         if ((threadIdx.x & 63u) == 0) {
             stats[2 * i] = v.mean;
             stats[2 * i + 1] = v.rstd;
@@ -454,7 +532,10 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_apply(NormArgs a, Plan p, 
         return load_vector<T, EVEN>(src + (n > 0 ? (row0 + r) * a.channels : 0), n);
     };
     Line l = parameters_of(a, q);
-    apply_moments(&l, p, q, stats + 2ull * q.n * a.groups, 0);
+    apply_moments(&l, p, q, 0, [&](uint32_t g) {
+        const double *st = stats + ((uint64_t)q.n * a.groups + g) * 2;
+        return group_of(st[0], st[1]);
+    });
     if (F != kPlain) put_tail(a);
     // every thread of the workgroup goes round as often: the lanes of a quantisation group meet in put_outputs
     f32x8 next = fetch(beg);
@@ -544,10 +625,14 @@ template <uint32_t S> struct HeldCodes {
 };
 template <uint32_t T, uint32_t S> using HeldAs = typename std::conditional<S == kPlain, Held<T, S>, HeldCodes<S>>::type;
 
-// h = x * hr + hm, u = h * gamma + beta of a thread's channels.  ONE: all of a vector's channels are in one group.
-template <bool ONE> struct Channels { float hr[ONE ? 1 : 8], hm[ONE ? 1 : 8], gamma[8], beta[8]; };
+// h' = (x - mean) * hr of a thread's channels, with the mean rounded to fp32.  What that rounding loses, hm = h - h', is the same
+// for all of a group: it is put where the values are summed or used, so that nothing grows with the distance of the
+// mean from zero and no value pays for it.  u = h' * gamma + beta, with hm * gamma in beta; B = B' + hm * A, and h B = h' B + hm B,
+// of which the second part is put to A.  ONE: all of a vector's channels are in one group.
+template <bool ONE> struct Channels { float mean[ONE ? 1 : 8], hr[ONE ? 1 : 8], gamma[8], beta[8]; };
+__device__ __forceinline__ double lost_of(const double *st) { return ((double)(float)st[0] - st[0]) * st[1]; }
 template <bool ONE>
-__device__ __forceinline__ Channels<ONE> channels_of(const NormArgs &a, const Plan &p, const Place &q)
+__device__ __forceinline__ Channels<ONE> channels_of(const NormArgs &a, const Plan &p, const Place &q, float (&hm)[ONE ? 1 : 8])
 {
     Channels<ONE> c;
 #pragma unroll
@@ -558,27 +643,27 @@ __device__ __forceinline__ Channels<ONE> channels_of(const NormArgs &a, const Pl
             c.beta[k] = a.beta ? a.beta[q.c + k] : 0.0f;
         }
         if (k < (ONE ? 1 : 8)) {
-            c.hr[k] = c.hm[k] = 0.0f;
+            c.mean[k] = c.hr[k] = hm[k] = 0.0f;
             if (k < q.valid) {
                 const double *st = a.stats + ((uint64_t)q.n * a.groups + p.div_per.div(q.c + k)) * 2;
+                c.mean[k] = (float)st[0];
                 c.hr[k] = (float)st[1];
-                c.hm[k] = (float)(-st[0] * st[1]);
+                hm[k] = (float)lost_of(st);
             }
         }
+        c.beta[k] = __builtin_fmaf(hm[ONE ? 0 : k], c.gamma[k], c.beta[k]);
     }
     return c;
 }
 
-// du = dy * act'(u) and h of eight channels.
+// du = dy * act'(u) and h' of eight channels.  in: the position exists; h' of the zero that stands for one may be infinite.
 template <uint32_t ACT, bool ONE>
 __device__ __forceinline__ void gradient8(const NormArgs &a, const Plan &p, const Place &q, const Channels<ONE> &c, const Source &x,
-                                          f32x8 dy, f32x8 *du, f32x8 *h)
+                                          f32x8 dy, f32x8 *du, f32x8 *h, bool in = true)
 {
-    const float one = x.s * c.hr[0];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const float hr = ONE ? one : x.s * c.hr[ONE ? 0 : k], hm = c.hm[ONE ? 0 : k];
-        const float hk = __builtin_fmaf(x.v[k], hr, hm);
+        const float hk = __builtin_fmaf(x.v[k], x.s, -c.mean[ONE ? 0 : k]) * (in ? c.hr[ONE ? 0 : k] : 0.0f);
         (*h)[k] = hk;
         if constexpr (ACT == kActNone) {
             (*du)[k] = dy[k];
@@ -589,15 +674,14 @@ __device__ __forceinline__ void gradient8(const NormArgs &a, const Plan &p, cons
                 (*du)[k] = dy[k] * (g * __builtin_fmaf(u, 1.0f - g, 1.0f));
             } else {
                 bool positive = u > 0.0f;
-                // where fp32 cannot tell the side of the border (its error is below eight roundings of these terms), fp64 does
-                const float terms = __builtin_fmaf(fabsf(c.gamma[k]), __builtin_fmaf(fabsf(x.v[k]), fabsf(hr), fabsf(hm)), fabsf(c.beta[k]));
+                // where fp32 cannot tell the side of the border (its error is below four roundings of these terms), fp64 does
+                const float terms = __builtin_fmaf(fabsf(c.gamma[k]), fabsf(hk), fabsf(c.beta[k]));
                 if (fabsf(u) < 0x1p-20f * terms && k < q.valid) {
-                    float gamma = c.gamma[k], beta = c.beta[k];
                     uint32_t ch = q.c + k;
-                    asm volatile("" : "+v"(gamma), "+v"(beta), "+v"(ch));   // rare: nothing of this is worth registers outside
+                    asm volatile("" : "+v"(ch));                           // rare: nothing of this is worth registers outside
                     const double *st = a.stats + ((uint64_t)q.n * a.groups + p.div_per.div(ch)) * 2;
-                    const double v = (double)x.v[k] * (double)x.s;
-                    positive = (v - st[0]) * st[1] * (double)gamma + (double)beta > 0.0;
+                    const double v = ((double)x.v[k] * (double)x.s - st[0]) * st[1];
+                    positive = v * (a.gamma ? (double)a.gamma[ch] : 1.0) + (a.beta ? (double)a.beta[ch] : 0.0) > 0.0;
                 }
                 (*du)[k] = positive ? dy[k] : u != u ? u : 0.0f;
             }
@@ -605,15 +689,24 @@ __device__ __forceinline__ void gradient8(const NormArgs &a, const Plan &p, cons
     }
 }
 
-// gamma of the segment's channels in LDS, for the waves that add up groups (a barrier follows).
+// gamma and hm of the segment's channels in LDS, for the waves that add up groups (a barrier follows).  ONE: hm once per vector,
+// whose threads put hm * A to their own sums; eight registers for it in the others spill.
+template <bool ONE> struct Shared {
+    const float *gamma, *lost;
+    __device__ __forceinline__ float hm(uint32_t c) const { return lost[ONE ? c >> 3 : c]; }
+};
 template <bool ONE>
-__device__ __forceinline__ const float *put_gamma(float *s, const Plan &p, const Place &q, const Channels<ONE> &c)
+__device__ __forceinline__ Shared<ONE> put_channels(float *s, const Plan &p, const Channels<ONE> &c, const float (&hm)[ONE ? 1 : 8])
 {
     if (threadIdx.x < p.nv) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s[8u * threadIdx.x + k] = c.gamma[k];
+        for (int k = 0; k < 8; ++k) {
+            s[8u * threadIdx.x + k] = c.gamma[k];
+            if (!ONE) s[8u * (p.nv + threadIdx.x) + k] = hm[ONE ? 0 : k];
+        }
+        if (ONE) s[8u * p.nv + threadIdx.x] = hm[0];
     }
-    return s;
+    return {s, s + 8u * p.nv};
 }
 
 __device__ __forceinline__ void add_sums(f32x8 du, f32x8 h, float (&sp)[8], float (&sq)[8])
@@ -625,7 +718,7 @@ __device__ __forceinline__ void add_sums(f32x8 du, f32x8 h, float (&sp)[8], floa
     }
 }
 
-// dx = hr * (du * gamma - (A + h * B)); ga, gb: A and B of the channels' groups, divided by the count.
+// dx = hr * (du * gamma - (A + h * B)); ga, gb: A + hm B and B of the channels' groups, divided by the count; h: h'.
 template <bool ONE>
 __device__ __forceinline__ f32x8 input_gradient(const Channels<ONE> &c, f32x8 du, f32x8 h, const float (&ga)[ONE ? 1 : 8],
                                                 const float (&gb)[ONE ? 1 : 8])
@@ -639,7 +732,7 @@ __device__ __forceinline__ f32x8 input_gradient(const Channels<ONE> &c, f32x8 du
     return dx;
 }
 
-// A and B over the count, for a thread's channels, from s[2 * g], s[2 * g + 1]; channel `first` is the first group's.
+// A + hm B and B over the count, for a thread's channels, from s[2 * g], s[2 * g + 1]; channel `first` is the first group's.
 template <bool ONE>
 __device__ __forceinline__ void pick_totals(const double *s, const NormArgs &a, const Plan &p, const Place &q, uint32_t first,
                                             float (&ga)[ONE ? 1 : 8], float (&gb)[ONE ? 1 : 8])
@@ -710,7 +803,9 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_slab(NormArgs a, Plan
     const uint32_t first = q.chunk * p.nv * 8u, end = a.channels - first < p.nv * 8u ? a.channels : first + p.nv * 8u;
     q = place(p, blockIdx.x, first, end);
     const uint64_t row0 = (uint64_t)q.n * a.spatial;
-    const Channels<ONE> ch = channels_of<ONE>(a, p, q);
+    float *s = reinterpret_cast<float *>(s_sum);
+    float hm[ONE ? 1 : 8];
+    const Channels<ONE> ch = channels_of<ONE>(a, p, q, hm);
     Held<T, kPlain> dy[kSlabRows];
     HeldAs<T, S> x[kSlabRows];
 #pragma unroll
@@ -720,6 +815,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_slab(NormArgs a, Plan
         dy[i].template load<ONE>(a.dy, a, row0 + r, q.c, n);
         x[i].template load<ONE>(a.x, a, row0 + r, q.c, n);
     }
+    const Shared<ONE> sc = put_channels<ONE>(s + blockDim.x * 16u, p, ch, hm);
     float sp[8], sq[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) sp[k] = sq[k] = 0.0f;
@@ -727,28 +823,32 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_slab(NormArgs a, Plan
 #pragma unroll
     for (uint32_t i = 0; i < kSlabRows; ++i) {
         if (i * p.rp >= a.spatial) break;                                 // (uniform)
-        gradient8<ACT, ONE>(a, p, q, ch, x[i].values(), dy[i].values().v, &du, &h);
+        gradient8<ACT, ONE>(a, p, q, ch, x[i].values(), dy[i].values().v, &du, &h, q.r + i * p.rp < a.spatial);
         add_sums(du, h, sp, sq);
     }
-    float *s = reinterpret_cast<float *>(s_sum);
-    double *tot = s_sum + 8u * blockDim.x + 4u * p.nv;
-    const float *s2 = s + blockDim.x * 8u, *sg = put_gamma(s + blockDim.x * 16u, p, q, ch);
+    double *tot = s_sum + 8u * blockDim.x + 8u * p.nv;
+    const float *s2 = s + blockDim.x * 8u;
+    auto sum_h = [&](uint32_t c) { return ONE ? s2[c] : __builtin_fmaf(sc.hm(c), s[c], s2[c]); };   // of du * h
+    if (ONE) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sq[k] = __builtin_fmaf(hm[0], sp[k], sq[k]);
+    }
     join_channels(s, sp, sq, p);
     const uint32_t groups = (end - first) / p.per, w = lanes_of(p.per);
     for (uint32_t c = threadIdx.x; c < end - first; c += blockDim.x) {
         if (a.batch == 1) {
             if (a.dbeta) a.dbeta[first + c] = s[c];
-            if (a.dgamma) a.dgamma[first + c] = s2[c];
+            if (a.dgamma) a.dgamma[first + c] = sum_h(c);
         } else {
             float *chan = static_cast<float *>(a.work) + 2ull * q.n * a.channels + first + c;
             chan[0] = s[c];
-            chan[a.channels] = s2[c];
+            chan[a.channels] = sum_h(c);
         }
     }
     each_group(groups, w, [&](uint32_t g, uint32_t sub, bool mine) {
-        const double t1 = group_total(g, p.per, sub, w, [&](uint32_t c) { return (double)s[c] * (double)sg[c]; });
-        const double t2 = group_total(g, p.per, sub, w, [&](uint32_t c) { return (double)s2[c] * (double)sg[c]; });
-        if (mine) { tot[2 * g] = t1; tot[2 * g + 1] = t2; }
+        const double t1 = group_total(g, p.per, sub, w, [&](uint32_t c) { return (double)s[c] * (double)sc.gamma[c]; });
+        const double t2 = group_total(g, p.per, sub, w, [&](uint32_t c) { return (double)sum_h(c) * (double)sc.gamma[c]; });
+        if (mine) { tot[2 * g] = t1 + (double)sc.hm(g * p.per) * t2; tot[2 * g + 1] = t2; }
     });
     __syncthreads();
     float ga[ONE ? 1 : 8], gb[ONE ? 1 : 8];
@@ -802,30 +902,37 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_sums(NormArgs a, Plan
 {
     extern __shared__ double s_sum[];
     const Place q = place(p, blockIdx.x, 0, a.channels);
-    const Channels<ONE> ch = channels_of<ONE>(a, p, q);
+    float *s = reinterpret_cast<float *>(s_sum);
+    float hm[ONE ? 1 : 8];
+    const Channels<ONE> ch = channels_of<ONE>(a, p, q, hm);
+    const Shared<ONE> sc = put_channels<ONE>(s + blockDim.x * 16u, p, ch, hm);
     float sp[8], sq[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) sp[k] = sq[k] = 0.0f;
     each_gradient<T, S, ACT, ONE>(a, p, q, ch, [&](uint64_t, f32x8 du, f32x8 h) { add_sums(du, h, sp, sq); });
-    float *s = reinterpret_cast<float *>(s_sum);
-    const float *s2 = s + blockDim.x * 8u, *sg = put_gamma(s + blockDim.x * 16u, p, q, ch);
+    const float *s2 = s + blockDim.x * 8u;
+    auto sum_h = [&](uint32_t c) { return ONE ? s2[c] : __builtin_fmaf(sc.hm(c), s[c], s2[c]); };   // of du * h
+    if (ONE) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sq[k] = __builtin_fmaf(hm[0], sp[k], sq[k]);
+    }
     join_channels(s, sp, sq, p);
     const uint32_t w = lanes_of(p.per);
     double *part = static_cast<double *>(a.work);
     float *chan = reinterpret_cast<float *>(part + 2ull * a.batch * a.groups * p.chunks) + 2ull * blockIdx.x * a.channels;
     for (uint32_t c = threadIdx.x; c < a.channels; c += blockDim.x) {
         chan[c] = s[c];
-        chan[a.channels + c] = s2[c];
+        chan[a.channels + c] = sum_h(c);
     }
     each_group(a.groups, w, [&](uint32_t g, uint32_t sub, bool mine) {
-        const double t1 = group_total(g, p.per, sub, w, [&](uint32_t c) { return (double)s[c] * (double)sg[c]; });
-        const double t2 = group_total(g, p.per, sub, w, [&](uint32_t c) { return (double)s2[c] * (double)sg[c]; });
+        const double t1 = group_total(g, p.per, sub, w, [&](uint32_t c) { return (double)s[c] * (double)sc.gamma[c]; });
+        const double t2 = group_total(g, p.per, sub, w, [&](uint32_t c) { return (double)sum_h(c) * (double)sc.gamma[c]; });
         double *o = part + (((uint64_t)q.n * a.groups + g) * p.chunks + q.chunk) * 2;
         if (mine) { o[0] = t1; o[1] = t2; }
     });
 }
 
-// Between the two passes: the totals A and B of every sample and group, and the parameters' gradients.
+// Between the two passes: the totals A + hm B and B of every sample and group, and the parameters' gradients.
 __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_join(NormArgs a, Plan p, double *totals, uint32_t param_blocks)
 {
     extern __shared__ double s_sum[];
@@ -839,7 +946,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_join(NormArgs a, Plan
     for (uint64_t i = (blockIdx.x - param_blocks) * 16ull + (threadIdx.x >> 6); i < a.batch * a.groups; i += step) {
         const Totals t = join_chunks(part, i, p);
         if ((threadIdx.x & 63u) == 0) {
-            totals[2 * i] = t.t1;
+            totals[2 * i] = t.t1 + lost_of(a.stats + 2 * i) * t.t2;
             totals[2 * i + 1] = t.t2;
         }
     }
@@ -850,7 +957,8 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_apply(NormArgs a, Pla
 {
     typedef typename ElemOf<T>::type E;
     const Place q = place(p, blockIdx.x, 0, a.channels);
-    const Channels<ONE> ch = channels_of<ONE>(a, p, q);
+    float hm[ONE ? 1 : 8];
+    const Channels<ONE> ch = channels_of<ONE>(a, p, q, hm);
     float ga[ONE ? 1 : 8], gb[ONE ? 1 : 8];
     pick_totals<ONE>(totals + 2ull * q.n * a.groups, a, p, q, 0, ga, gb);
     each_gradient<T, S, ACT, ONE>(a, p, q, ch, [&](uint64_t row, f32x8 du, f32x8 h) {
@@ -904,7 +1012,7 @@ void backward_as(const NormArgs &a, hipStream_t st)
     Plan p;
     if (a.batch && slab_plan(&p, a, 1)) {
         hipLaunchKernelGGL((k_norm_grad_slab<T, S, ACT, ONE>), dim3((uint32_t)(a.batch * p.chunks)), dim3(p.threads),
-                           lds_bytes(p, 64, p.nv * 8u / p.per, true) + 32 * p.nv, st, a, p);
+                           lds_bytes(p, 64, p.nv * 8u / p.per, true) + 64 * p.nv, st, a, p);
         if (!params || a.batch == 1) return;
         const float *chan = static_cast<const float *>(a.work);
         uint64_t records = a.batch;
@@ -926,7 +1034,7 @@ void backward_as(const NormArgs &a, hipStream_t st)
     double *totals = reinterpret_cast<double *>(static_cast<uint8_t *>(a.work) + records_bytes(a, p, true));
     const uint32_t joins = work ? join_blocks(a) : 0;
     if (work)
-        hipLaunchKernelGGL((k_norm_grad_sums<T, S, ACT, ONE>), dim3(work), dim3(p.threads), lds_bytes(p, 64, 0, false) + 32 * p.nv, st, a, p);
+        hipLaunchKernelGGL((k_norm_grad_sums<T, S, ACT, ONE>), dim3(work), dim3(p.threads), lds_bytes(p, 64, 0, false) + 64 * p.nv, st, a, p);
     if (params + joins)
         hipLaunchKernelGGL(k_norm_grad_join, dim3(params + joins), dim3(kMaxThreads), 8 * kMaxThreads, st, a, p, totals, params);
     if (work) hipLaunchKernelGGL((k_norm_grad_apply<T, S, ACT, ONE>), dim3(work), dim3(p.threads), 0, st, a, p, totals);
