@@ -359,7 +359,7 @@ __device__ __forceinline__ void put_tail(const NormArgs &a)
 template <uint32_t T, uint32_t F, bool EVEN>
 __global__ __launch_bounds__(kMaxThreads) void k_norm_slab(NormArgs a, Plan p)
 {
-    extern __shared__ double s_sum[];
+    extern __shared__ __align__(16) double s_sum[];
     __shared__ uint32_t s_unsure;
     typedef typename ElemOf<T>::type E;
     Place q = place(p, blockIdx.x, 0, 0);
@@ -433,7 +433,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_slab(NormArgs a, Plan p)
 template <uint32_t T, bool EVEN>
 __global__ __launch_bounds__(kMaxThreads) void k_norm_sums(NormArgs a, Plan p)
 {
-    extern __shared__ double s_sum[];
+    extern __shared__ __align__(16) double s_sum[];
     __shared__ uint32_t s_unsure;
     typedef typename ElemOf<T>::type E;
     const Place q = place(p, blockIdx.x, 0, a.channels);
@@ -779,7 +779,7 @@ __device__ __forceinline__ void join_parameters(double *s, const NormArgs &a, co
 __global__ __launch_bounds__(kMaxThreads) void k_norm_parameters(NormArgs a, const float *chan, uint64_t records, uint64_t range,
                                                                  uint32_t blocks, float *to)
 {
-    extern __shared__ double s_sum[];
+    extern __shared__ __align__(16) double s_sum[];
     const uint32_t r = blockIdx.x / blocks, block = blockIdx.x - r * blocks;
     const uint64_t beg = r * range, n = records - beg < range ? records - beg : range;
     float *out = to + 2ull * r * a.channels;
@@ -797,7 +797,7 @@ uint32_t parameter_ranges(const NormArgs &a, uint64_t records)
 template <uint32_t T, uint32_t S, uint32_t ACT, bool ONE>
 __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_slab(NormArgs a, Plan p)
 {
-    extern __shared__ double s_sum[];
+    extern __shared__ __align__(16) double s_sum[];
     typedef typename ElemOf<T>::type E;
     Place q = place(p, blockIdx.x, 0, 0);
     const uint32_t first = q.chunk * p.nv * 8u, end = a.channels - first < p.nv * 8u ? a.channels : first + p.nv * 8u;
@@ -900,7 +900,7 @@ __device__ __forceinline__ void each_gradient(const NormArgs &a, const Plan &p, 
 template <uint32_t T, uint32_t S, uint32_t ACT, bool ONE>
 __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_sums(NormArgs a, Plan p)
 {
-    extern __shared__ double s_sum[];
+    extern __shared__ __align__(16) double s_sum[];
     const Place q = place(p, blockIdx.x, 0, a.channels);
     float *s = reinterpret_cast<float *>(s_sum);
     float hm[ONE ? 1 : 8];
@@ -935,7 +935,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_sums(NormArgs a, Plan
 // Between the two passes: the totals A + hm B and B of every sample and group, and the parameters' gradients.
 __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_join(NormArgs a, Plan p, double *totals, uint32_t param_blocks)
 {
-    extern __shared__ double s_sum[];
+    extern __shared__ __align__(16) double s_sum[];
     const double *part = static_cast<const double *>(a.work);
     if (blockIdx.x < param_blocks) {
         join_parameters(s_sum, a, reinterpret_cast<const float *>(part + 2ull * a.batch * a.groups * p.chunks),
