@@ -101,7 +101,10 @@ bool slab_plan(Plan *out, const NormArgs &a, uint32_t lanes)
     uint32_t rows = (uint32_t)((vectors + kMaxThreads - 1) / kMaxThreads);
     if (a.batch * p.chunks * vectors > 256ull * kMaxThreads && rows < kSlabRows) rows = kSlabRows;
     p.rp = (a.spatial + rows - 1) / rows;
-    while ((uint64_t)p.rp * p.nv > kMaxThreads) p.rp = (a.spatial + ++rows - 1) / rows;
+    while ((uint64_t)p.rp * p.nv > kMaxThreads) {
+        ++rows;
+        p.rp = (a.spatial + rows - 1) / rows;
+    }
     if (rows > kSlabRows) return false;
     p.rows_per = a.spatial;
     finish_plan(&p, a);
