@@ -361,7 +361,10 @@ int cmp_byte_linear_grad(int device, const cmp_byte_shape *shape, const void *d_
  * d_gamma, d_beta: fp32, one per channel, either may be NULL (ones, zeros).  d_stats (double, [batch][groups][2]: mean,
  * 1 / sqrt(var + eps)) is written for the backward pass; NULL: not wanted.  With d_ck the input is kept as a byte
  * checkpoint of batch * spatial rows in the same pass, the bytes of cmp_byte_store; NULL: not kept.
- * d_work: cmp_group_norm_work bytes (it may be 0), aligned to 16, used during a call only, the same for both directions.
+ * d_work: aligned to 16, used during a call only, its bytes may be 0.  cmp_group_norm takes cmp_group_norm_work bytes, which are
+ * enough for either direction, so that one buffer serves both.  cmp_group_norm_forward is the same call with the bytes that
+ * this direction uses, cmp_group_norm_forward_work (`group`: the checkpoint's, 0 without one; 0 bytes on another); the backward
+ * pass takes cmp_group_norm_grad_work bytes (`params`: d_dgamma or d_dbeta is given, whose sums take most of them).
  * cmp_group_norm_grad takes the input d_x OR its checkpoint d_ck (the other NULL), gamma, beta and d_stats of
  * the forward pass, and gives, with u = h * gamma + beta from the restored input and du = dy * act'(u),
  *    dbeta = sum du,  dgamma = sum du * h   (fp32, overwritten; either may be NULL)
@@ -387,9 +390,14 @@ typedef struct {
 } cmp_norm_shape;
 
 size_t cmp_group_norm_work(const cmp_norm_shape *shape);
+size_t cmp_group_norm_forward_work(const cmp_norm_shape *shape, uint32_t group);
+size_t cmp_group_norm_grad_work(const cmp_norm_shape *shape, int params);
 int cmp_group_norm(int device, const cmp_norm_shape *shape, const void *d_x, const float *d_gamma, const float *d_beta, void *d_y,
                    double *d_stats, uint32_t format, uint32_t group, void *d_ck, size_t cap, void *d_work, size_t work_bytes,
                    void *stream);
+int cmp_group_norm_forward(int device, const cmp_norm_shape *shape, const void *d_x, const float *d_gamma, const float *d_beta, void *d_y,
+                           double *d_stats, uint32_t format, uint32_t group, void *d_ck, size_t cap, void *d_work, size_t work_bytes,
+                           void *stream);
 int cmp_group_norm_grad(int device, const cmp_norm_shape *shape, const void *d_dy, const void *d_x, uint32_t format, uint32_t group,
                         const void *d_ck, size_t bytes, const float *d_gamma, const float *d_beta, const double *d_stats, void *d_dx,
                         float *d_dgamma, float *d_dbeta, void *d_work, size_t work_bytes, void *stream);

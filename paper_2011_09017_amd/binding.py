@@ -30,7 +30,8 @@ EXPORTS = ["cmp_default_config", "cmp_create", "cmp_destroy", "cmp_bound", "cmp_
            "cmp_compress_begin", "cmp_compress_finish", "cmp_compress_batch", "cmp_decompress_batch", "cmp_compress_static",
            "cmp_arena_state_bytes", "cmp_arena_accepts", "cmp_arena_init", "cmp_arena_push", "cmp_arena_pop", "cmp_arena_stats",
            "cmp_byte_bytes", "cmp_byte_store", "cmp_byte_load", "cmp_byte_linear_grad_work", "cmp_byte_linear_grad",
-           "cmp_group_norm_work", "cmp_group_norm", "cmp_group_norm_grad"]
+           "cmp_group_norm_work", "cmp_group_norm", "cmp_group_norm_grad", "cmp_group_norm_forward_work", "cmp_group_norm_forward",
+           "cmp_group_norm_grad_work"]
 
 
 class cmp_controller_config(C.Structure):
@@ -100,7 +101,10 @@ def lib() -> C.CDLL:
         L.cmp_byte_linear_grad.argtypes = [i32, vp, vp, sz, vp, u32, u64, u64, vp, vp, u32, i32, vp, sz, vp]
         L.cmp_byte_linear_grad.restype = i32
         L.cmp_group_norm_work.argtypes = [vp]; L.cmp_group_norm_work.restype = sz
-        L.cmp_group_norm.argtypes = [i32, vp, vp, vp, vp, vp, vp, u32, u32, vp, sz, vp, sz, vp]; L.cmp_group_norm.restype = i32
+        L.cmp_group_norm_forward_work.argtypes = [vp, u32]; L.cmp_group_norm_forward_work.restype = sz
+        L.cmp_group_norm_grad_work.argtypes = [vp, i32]; L.cmp_group_norm_grad_work.restype = sz
+        for f in (L.cmp_group_norm, L.cmp_group_norm_forward):
+            f.argtypes = [i32, vp, vp, vp, vp, vp, vp, u32, u32, vp, sz, vp, sz, vp]; f.restype = i32
         L.cmp_group_norm_grad.argtypes = [i32, vp, vp, vp, u32, u32, vp, sz, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.cmp_group_norm_grad.restype = i32
         _lib = L
@@ -306,6 +310,20 @@ def cmp_group_norm(device: int, shape: cmp_norm_shape, d_x: int, d_gamma, d_beta
                    cap: int, d_work: int, work_bytes: int, stream: int) -> int:
     return lib().cmp_group_norm(device, C.addressof(shape), d_x, d_gamma, d_beta, d_y, d_stats, format, group, d_ck, cap, d_work,
                                 work_bytes, stream)
+
+
+def cmp_group_norm_forward_work(shape: cmp_norm_shape, group: int) -> int:
+    return int(lib().cmp_group_norm_forward_work(C.addressof(shape), group))
+
+
+def cmp_group_norm_forward(device: int, shape: cmp_norm_shape, d_x: int, d_gamma, d_beta, d_y: int, d_stats, format: int, group: int,
+                           d_ck, cap: int, d_work: int, work_bytes: int, stream: int) -> int:
+    return lib().cmp_group_norm_forward(device, C.addressof(shape), d_x, d_gamma, d_beta, d_y, d_stats, format, group, d_ck, cap,
+                                        d_work, work_bytes, stream)
+
+
+def cmp_group_norm_grad_work(shape: cmp_norm_shape, params: bool) -> int:
+    return int(lib().cmp_group_norm_grad_work(C.addressof(shape), 1 if params else 0))
 
 
 def cmp_group_norm_grad(device: int, shape: cmp_norm_shape, d_dy: int, d_x, format: int, group: int, d_ck, nbytes: int, d_gamma,

@@ -242,7 +242,9 @@ struct NormArgs {
     uint32_t       spatial, channels, groups, type, act, format, gshift;
     double         eps;
 };
-uint64_t group_norm_work(const NormArgs &a);
+uint64_t group_norm_work(const NormArgs &a);                               // enough for either direction in any of its forms
+uint64_t group_norm_forward_work(const NormArgs &a, uint32_t group);       // columns of a scale of the checkpoint, 0: none
+uint64_t group_norm_grad_work(const NormArgs &a, bool params);
 void launch_group_norm(const NormArgs &a, hipStream_t st);
 void launch_group_norm_grad(const NormArgs &a, hipStream_t st);
 

@@ -106,6 +106,34 @@ int norm_checkpoint(NormArgs *a, const cmp_norm_shape &s, uint32_t format, uint3
     return rc;
 }
 
+int norm_forward(int device, const cmp_norm_shape *shape, const void *d_x, const float *d_gamma, const float *d_beta, void *d_y,
+                 double *d_stats, uint32_t format, uint32_t group, void *d_ck, size_t cap, void *d_work, size_t work_bytes,
+                 void *stream, bool either)
+{
+    NormArgs a;
+    int rc = norm_args(&a, shape);
+    if (rc != CMP_OK) return rc;
+    const bool empty = shape->batch == 0 || shape->spatial == 0;
+    const uint32_t es = type_bytes(shape->type);
+    if (!empty && (!d_x || !d_y || misaligned(d_x, es) || misaligned(d_y, es))) return CMP_E_ARG;
+    if (misaligned(d_gamma, 4) || misaligned(d_beta, 4) || misaligned(d_stats, 8)) return CMP_E_ARG;
+    if (d_ck && (rc = norm_checkpoint(&a, *shape, format, group, d_ck, cap, CMP_E_NOSPACE)) != CMP_OK) return rc;
+    const uint64_t need = empty ? 0 : either ? group_norm_work(a) : group_norm_forward_work(a, d_ck ? group : 0);
+    if (work_bytes < need) return CMP_E_NOSPACE;
+    if (need && (!d_work || misaligned(d_work, 16))) return CMP_E_ARG;
+    DeviceGuard guard(device);
+    if (guard.rc != CMP_OK) return guard.rc;
+    if (empty) return CMP_OK;
+    a.x = d_x;
+    a.y = d_y;
+    a.gamma = d_gamma;
+    a.beta = d_beta;
+    a.stats = d_stats;
+    a.work = d_work;
+    launch_group_norm(a, static_cast<hipStream_t>(stream));
+    return launched();
+}
+
 }  // namespace
 
 extern "C" {
@@ -190,32 +218,32 @@ size_t cmp_group_norm_work(const cmp_norm_shape *shape)
     return a.batch && a.spatial ? (size_t)group_norm_work(a) : 0;
 }
 
+size_t cmp_group_norm_forward_work(const cmp_norm_shape *shape, uint32_t group)
+{
+    NormArgs a;
+    if (norm_args(&a, shape) != CMP_OK || (group != 0 && group != 32 && group != 64 && group != 128)) return 0;
+    return a.batch && a.spatial ? (size_t)group_norm_forward_work(a, group) : 0;
+}
+
+size_t cmp_group_norm_grad_work(const cmp_norm_shape *shape, int params)
+{
+    NormArgs a;
+    if (norm_args(&a, shape) != CMP_OK) return 0;
+    return a.batch && a.spatial ? (size_t)group_norm_grad_work(a, params != 0) : 0;
+}
+
 int cmp_group_norm(int device, const cmp_norm_shape *shape, const void *d_x, const float *d_gamma, const float *d_beta, void *d_y,
                    double *d_stats, uint32_t format, uint32_t group, void *d_ck, size_t cap, void *d_work, size_t work_bytes,
                    void *stream)
 {
-    NormArgs a;
-    int rc = norm_args(&a, shape);
-    if (rc != CMP_OK) return rc;
-    const bool empty = shape->batch == 0 || shape->spatial == 0;
-    const uint32_t es = type_bytes(shape->type);
-    if (!empty && (!d_x || !d_y || misaligned(d_x, es) || misaligned(d_y, es))) return CMP_E_ARG;
-    if (misaligned(d_gamma, 4) || misaligned(d_beta, 4) || misaligned(d_stats, 8)) return CMP_E_ARG;
-    if (d_ck && (rc = norm_checkpoint(&a, *shape, format, group, d_ck, cap, CMP_E_NOSPACE)) != CMP_OK) return rc;
-    const uint64_t need = empty ? 0 : group_norm_work(a);
-    if (work_bytes < need) return CMP_E_NOSPACE;
-    if (need && (!d_work || misaligned(d_work, 16))) return CMP_E_ARG;
-    DeviceGuard guard(device);
-    if (guard.rc != CMP_OK) return guard.rc;
-    if (empty) return CMP_OK;
-    a.x = d_x;
-    a.y = d_y;
-    a.gamma = d_gamma;
-    a.beta = d_beta;
-    a.stats = d_stats;
-    a.work = d_work;
-    launch_group_norm(a, static_cast<hipStream_t>(stream));
-    return launched();
+    return norm_forward(device, shape, d_x, d_gamma, d_beta, d_y, d_stats, format, group, d_ck, cap, d_work, work_bytes, stream, true);
+}
+
+int cmp_group_norm_forward(int device, const cmp_norm_shape *shape, const void *d_x, const float *d_gamma, const float *d_beta, void *d_y,
+                           double *d_stats, uint32_t format, uint32_t group, void *d_ck, size_t cap, void *d_work, size_t work_bytes,
+                           void *stream)
+{
+    return norm_forward(device, shape, d_x, d_gamma, d_beta, d_y, d_stats, format, group, d_ck, cap, d_work, work_bytes, stream, false);
 }
 
 int cmp_group_norm_grad(int device, const cmp_norm_shape *shape, const void *d_dy, const void *d_x, uint32_t format, uint32_t group,
@@ -233,7 +261,7 @@ int cmp_group_norm_grad(int device, const cmp_norm_shape *shape, const void *d_d
         misaligned(d_dbeta, 4))
         return CMP_E_ARG;
     if (d_ck && (rc = norm_checkpoint(&a, *shape, format, group, d_ck, bytes, CMP_E_FORMAT)) != CMP_OK) return rc;
-    const uint64_t need = empty ? 0 : group_norm_work(a);
+    const uint64_t need = empty ? 0 : group_norm_grad_work(a, d_dgamma || d_dbeta);
     if (work_bytes < need) return CMP_E_NOSPACE;
     if (need && (!d_work || misaligned(d_work, 16))) return CMP_E_ARG;
     DeviceGuard guard(device);

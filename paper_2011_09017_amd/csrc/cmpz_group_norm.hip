@@ -838,7 +838,8 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_slab(NormArgs a, Plan
     }
     join_channels(s, sp, sq, p);
     const uint32_t groups = (end - first) / p.per, w = lanes_of(p.per);
-    for (uint32_t c = threadIdx.x; c < end - first; c += blockDim.x) {
+    const bool params = a.dbeta || a.dgamma;
+    for (uint32_t c = threadIdx.x; params && c < end - first; c += blockDim.x) {
         if (a.batch == 1) {
             if (a.dbeta) a.dbeta[first + c] = s[c];
             if (a.dgamma) a.dgamma[first + c] = sum_h(c);
@@ -923,7 +924,8 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_grad_sums(NormArgs a, Plan
     const uint32_t w = lanes_of(p.per);
     double *part = static_cast<double *>(a.work);
     float *chan = reinterpret_cast<float *>(part + 2ull * a.batch * a.groups * p.chunks) + 2ull * blockIdx.x * a.channels;
-    for (uint32_t c = threadIdx.x; c < a.channels; c += blockDim.x) {
+    const bool params = a.dbeta || a.dgamma;
+    for (uint32_t c = threadIdx.x; params && c < a.channels; c += blockDim.x) {
         chan[c] = s[c];
         chan[a.channels + c] = sum_h(c);
     }
@@ -982,18 +984,20 @@ uint32_t join_blocks(const NormArgs &a)                                   // six
     const uint64_t n = (a.batch * a.groups + kMaxThreads / 64 - 1) / (kMaxThreads / 64);
     return (uint32_t)(n < 65536 ? n : 65536);
 }
-// What the first pass leaves in the workspace: two totals per sample, range and group; backward: two sums per channel behind them.
-uint64_t records_bytes(const NormArgs &a, const Plan &p, bool backward)
+// What the first pass leaves in the workspace: two totals per sample, range and group; for the parameters' gradients two sums
+// per channel behind them.
+uint64_t records_bytes(const NormArgs &a, const Plan &p, bool params)
 {
     const uint64_t records = a.batch * p.chunks;
-    return (records * (16ull * a.groups + (backward ? 8ull * a.channels : 0ull)) + 15) & ~15ull;
+    return (records * (16ull * a.groups + (params ? 8ull * a.channels : 0ull)) + 15) & ~15ull;
 }
+uint32_t lanes_of_group(uint32_t group) { return group ? group / 8u : 1u; }   // threads of a position that share a scale
 size_t moment_bytes(const Plan &p) { return p.per < 8u ? 128 : 32; }
 
 template <uint32_t T, uint32_t F, bool EVEN>
 void forward_as(const NormArgs &a, hipStream_t st)
 {
-    const uint32_t lanes = F != kPlain ? 1u << (a.gshift - 3) : 1u;
+    const uint32_t lanes = lanes_of_group(F != kPlain ? 1u << a.gshift : 0u);
     Plan p;
     if (slab_plan(&p, a, lanes)) {
         hipLaunchKernelGGL((k_norm_slab<T, F, EVEN>), dim3((uint32_t)(a.batch * p.chunks)), dim3(p.threads),
@@ -1034,7 +1038,7 @@ void backward_as(const NormArgs &a, hipStream_t st)
     }
     p = two_pass_plan(a, 1);
     const uint32_t work = a.spatial ? (uint32_t)(a.batch * p.chunks) : 0;
-    double *totals = reinterpret_cast<double *>(static_cast<uint8_t *>(a.work) + records_bytes(a, p, true));
+    double *totals = reinterpret_cast<double *>(static_cast<uint8_t *>(a.work) + records_bytes(a, p, params != 0));
     const uint32_t joins = work ? join_blocks(a) : 0;
     if (work)
         hipLaunchKernelGGL((k_norm_grad_sums<T, S, ACT, ONE>), dim3(work), dim3(p.threads), lds_bytes(p, 64, 0, false) + 64 * p.nv, st, a, p);
@@ -1083,16 +1087,26 @@ void forward_of(const NormArgs &a, hipStream_t st)
 
 }  // namespace
 
-// One figure for a forward and a backward pass, with a checkpoint or without (the plans differ with the threads that a
-// position takes).
+uint64_t group_norm_forward_work(const NormArgs &a, uint32_t group)
+{
+    const uint32_t lanes = lanes_of_group(group);
+    Plan p;
+    if (slab_plan(&p, a, lanes)) return 0;
+    return records_bytes(a, two_pass_plan(a, lanes), false) + 16ull * a.batch * a.groups;   // and mean and deviation, if nobody wants them
+}
+
+uint64_t group_norm_grad_work(const NormArgs &a, bool params)
+{
+    Plan p;
+    if (slab_plan(&p, a, 1)) return params && a.batch > 1 ? 8ull * (a.batch + parameter_ranges(a, a.batch)) * a.channels : 0;   // sums of every sample
+    return records_bytes(a, two_pass_plan(a, 1), params) + 16ull * a.batch * a.groups;
+}
+
 uint64_t group_norm_work(const NormArgs &a)
 {
-    uint64_t most = 0;
-    for (uint32_t lanes : {1u, 4u, 8u, 16u}) {
-        Plan p;
-        uint64_t bytes;
-        if (slab_plan(&p, a, lanes)) bytes = lanes == 1u && a.batch > 1 ? 8ull * (a.batch + parameter_ranges(a, a.batch)) * a.channels : 0;   // sums of every sample
-        else bytes = records_bytes(a, two_pass_plan(a, lanes), lanes == 1u) + 16ull * a.batch * a.groups;
+    uint64_t most = group_norm_grad_work(a, true);
+    for (uint32_t group : {0u, 32u, 64u, 128u}) {
+        const uint64_t bytes = group_norm_forward_work(a, group);
         if (bytes > most) most = bytes;
     }
     return most;

@@ -197,18 +197,19 @@ def byte_linear_grad(dy: torch.Tensor, ck: ByteCheckpoint, bias: bool = False, d
 
 
 @lru_cache(maxsize=4096)
-def _norm_plan(batch: int, spatial: int, channels: int, groups: int, kind: int, act: str, eps: float):
+def _norm_plan(batch: int, spatial: int, channels: int, groups: int, kind: int, act: str, eps: float, backward: bool, part: int):
     """(the C shape, bytes of the workspace): depend on sizes only and are read only."""
     _refuse(not 0 <= groups < 1 << 32 or channels >= 1 << 32, f"group norm: {groups} groups of {channels} channels")   # fields of 32 bits
     shape = binding.cmp_norm_shape(batch, spatial, channels, groups, kind, _ACTS[act], eps)
-    return shape, binding.cmp_group_norm_work(shape)
+    return shape, (binding.cmp_group_norm_grad_work if backward else binding.cmp_group_norm_forward_work)(shape, part)
 
 
-def _norm_shape(x: torch.Tensor, groups: int, eps: float, act: str):
+def _norm_shape(x: torch.Tensor, groups: int, eps: float, act: str, backward: bool, part: int):
+    """part: forward the columns of a scale of the checkpoint, 0 without one; backward whether the parameters' gradients are wanted."""
     _refuse(act not in _ACTS, f"activation {act!r}: {', '.join(_ACTS)}")
     _refuse(x.dim() < 2, "group norm: [batch, ..., channels] is wanted")
     _refuse(not x.is_contiguous(), "group norm: a contiguous tensor is wanted, channels last")
-    return _norm_plan(x.shape[0], math.prod(x.shape[1:-1]), x.shape[-1], groups, _type_of(x), act, eps)
+    return _norm_plan(x.shape[0], math.prod(x.shape[1:-1]), x.shape[-1], groups, _type_of(x), act, eps, backward, part)
 
 
 def _parameter(t: Optional[torch.Tensor], channels: int, what: str):
@@ -223,7 +224,8 @@ def group_norm(x: torch.Tensor, groups: int, weight: Optional[torch.Tensor] = No
                eps: float = 1e-5, act: str = "none", save: Optional[str] = None, group: int = 64):
     """(y, stats, checkpoint) of x[batch, ..., channels]: y = act(group norm of x), act "none", "relu" or "silu"; stats is what
     :func:`group_norm_grad` needs; save="int8" or "e4m3" keeps x as a checkpoint (groups of `group` channels), else None."""
-    shape, need = _norm_shape(x, groups, eps, act)
+    _refuse(save is not None and group not in GROUPS, f"groups of {group}: 32, 64 or 128")
+    shape, need = _norm_shape(x, groups, eps, act, False, group if save is not None else 0)
     dev = _on_gpu(x, weight, bias)
     gamma, beta = _parameter(weight, x.shape[-1], "weight"), _parameter(bias, x.shape[-1], "bias")
     y = torch.empty_like(x)
@@ -234,9 +236,9 @@ def group_norm(x: torch.Tensor, groups: int, weight: Optional[torch.Tensor] = No
         fmt = held.format
         ck = ByteCheckpoint(torch.empty(nbytes, dtype=torch.uint8, device=dev), tuple(x.shape), x.dtype, save, group)
     work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    _call(binding.cmp_group_norm(dev.index, shape, x.data_ptr(), gamma, beta, y.data_ptr(), stats.data_ptr(), fmt, group,
-                                 None if ck is None else ck.buf.data_ptr(), 0 if ck is None else ck.buf.numel(),
-                                 None if work is None else work.data_ptr(), need, _stream(dev)), "cmp_group_norm")
+    _call(binding.cmp_group_norm_forward(dev.index, shape, x.data_ptr(), gamma, beta, y.data_ptr(), stats.data_ptr(), fmt, group,
+                                         None if ck is None else ck.buf.data_ptr(), 0 if ck is None else ck.buf.numel(),
+                                         None if work is None else work.data_ptr(), need, _stream(dev)), "cmp_group_norm")
     return y, stats, ck
 
 
@@ -244,7 +246,7 @@ def group_norm_grad(dy: torch.Tensor, x, stats: torch.Tensor, groups: int, weigh
                     bias: Optional[torch.Tensor] = None, act: str = "none", params: bool = True):
     """(dx, dweight, dbias) from dy, the input (a tensor of dy's type, or its :class:`ByteCheckpoint`), and what the forward
     pass was called with and gave.  params=False: the last two are None."""
-    shape, need = _norm_shape(dy, groups, 1.0, act)                   # eps is in stats
+    shape, need = _norm_shape(dy, groups, 1.0, act, True, bool(params))   # eps is in stats
     held = isinstance(x, ByteCheckpoint)
     src = x.buf if held else x
     dev = _on_gpu(dy, src, stats, weight, bias)

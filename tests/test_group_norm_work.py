@@ -1,0 +1,127 @@
+"""Workspaces of the group norm: a pass asks for what it writes, and writes no further."""
+import pytest
+import torch
+
+from paper_2011_09017_amd import binding as b, operators as ops
+
+P = 4096
+
+
+def _shape(batch, spatial, channels, groups, type=b.CMP_TYPE_BF, act=b.CMP_ACT_SILU):
+    return b.cmp_norm_shape(batch, spatial, channels, groups, type, act, 1e-5)
+
+
+def test_tokens_need_no_workspace_but_for_the_parameters():
+    """One pass: nothing lies between workgroups but the parameters' sums of every sample."""
+    s = _shape(65536, 1, 512, 32)
+    assert b.cmp_group_norm_forward_work(s, 0) == b.cmp_group_norm_forward_work(s, 128) == 0
+    assert b.cmp_group_norm_grad_work(s, False) == 0
+    assert b.cmp_group_norm_grad_work(s, True) >= 65536 * 512 * 8
+
+
+def test_two_passes_need_records_of_groups():
+    """A record of two doubles for each workgroup and group, mean and deviation of each sample and group; the parameters' sums
+    of every workgroup only where they are asked for."""
+    n, groups, channels = 8, 32, 320
+    s = _shape(n, 16384, channels, groups)
+    most = (n * 64 + n) * groups * 16                              # 512 workgroups
+    for work in [b.cmp_group_norm_forward_work(s, g) for g in (0, 32, 64, 128)] + [b.cmp_group_norm_grad_work(s, False)]:
+        assert n * groups * 16 * 2 <= work <= most
+    assert b.cmp_group_norm_grad_work(s, True) - b.cmp_group_norm_grad_work(s, False) >= 8 * channels * n
+    wide = _shape(1 << 21, 1, 8192, 128)                           # two passes although a sample is one position
+    assert b.cmp_group_norm_forward_work(wide, 0) <= 2 * 16 * (1 << 21) * 128 + 16
+
+
+@pytest.mark.parametrize("shape", [(2, 9, 24, 4), (8, 16384, 320, 32), (300, 4, 24, 2), (1, 49, 512, 32), (1, 4097, 320, 32), (1 << 10, 1, 8192, 128),
+                                   (3, 1500, 30, 10), (0, 5, 8, 2), (5, 0, 8, 2)])
+@pytest.mark.parametrize("type", [b.CMP_TYPE_F, b.CMP_TYPE_BF])
+def test_either_direction_fits_the_common_figure(shape, type):
+    s = _shape(*shape, type=type)
+    parts = [b.cmp_group_norm_forward_work(s, g) for g in (0, 32, 64, 128)] + [b.cmp_group_norm_grad_work(s, p) for p in (False, True)]
+    assert b.cmp_group_norm_work(s) == max(parts)
+    assert b.cmp_group_norm_grad_work(s, True) >= b.cmp_group_norm_grad_work(s, False)
+
+
+def test_refusals():
+    s = _shape(8, 16384, 320, 32)
+    bad = _shape(8, 16384, 320, 33)
+    assert b.cmp_group_norm_forward_work(bad, 0) == b.cmp_group_norm_grad_work(bad, True) == 0
+    assert b.cmp_group_norm_forward_work(s, 48) == 0
+    big = 1 << 40
+
+    def forward(s=s, group=64, ck=None, cap=big, work=P, need=big, x=P, y=P):
+        return b.cmp_group_norm_forward(0, s, x, None, None, y, None, 0, group, ck, cap, work, need, 0)
+    assert forward(bad) == forward(x=0) == forward(y=P + 1) == forward(work=0) == forward(work=P + 8) == forward(ck=P, group=48) == b.CMP_E_ARG
+    assert forward(need=b.cmp_group_norm_forward_work(s, 0) - 1) == b.CMP_E_NOSPACE
+    # rows of 100 channels take 13 vectors, with a checkpoint in groups of 128 columns 16: other ranges of positions
+    odd = _shape(1, 100000, 100, 1)
+    assert b.cmp_group_norm_forward_work(odd, 0) != b.cmp_group_norm_forward_work(odd, 128)
+    for group in (0, 128):
+        work = b.cmp_group_norm_forward_work(odd, group)
+        assert forward(odd, group, P if group else None, need=work - 1) == b.CMP_E_NOSPACE
+
+    def grad(dgamma, dbeta, need):
+        return b.cmp_group_norm_grad(0, s, P, P, 0, 64, None, 0, None, None, P, P, dgamma, dbeta, P, need, 0)
+    assert grad(None, None, b.cmp_group_norm_grad_work(s, False) - 1) == b.CMP_E_NOSPACE
+    for which in ((P, None), (None, P), (P, P)):
+        assert grad(*which, b.cmp_group_norm_grad_work(s, True) - 1) == b.CMP_E_NOSPACE
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch,spatial,channels,groups", [(8, 2000, 320, 32), (300, 4, 24, 2), (4096, 1, 512, 32), (1, 4097, 40, 5), (3, 1500, 30, 10),
+                                                           (1, 49, 512, 32), (2500, 1, 7, 7), (1, 20000, 100, 1)])
+@pytest.mark.parametrize("save,group", [(None, 0), ("int8", 32), ("e4m3", 128)])
+@pytest.mark.parametrize("far", [0.0, 3000.0])
+def test_a_pass_keeps_to_its_workspace(batch, spatial, channels, groups, save, group, far):
+    """Every call with exactly the bytes it asks for, in the middle of a buffer: what lies around them stays, and the results are
+    those of operators that have more.  far: also the sums that are taken twice."""
+    gen = torch.Generator().manual_seed(batch + spatial + channels)
+    x = (far + torch.randn(batch, spatial, channels, generator=gen)).cuda()
+    dy = torch.randn(batch, spatial, channels, generator=gen).cuda()
+    w, bias = torch.rand(channels, generator=gen).cuda() + 0.5, torch.randn(channels, generator=gen).cuda()
+    y, stats, ck = ops.group_norm(x, groups, w, bias, act="silu", save=save, group=group or 64)
+    dx, dw, db = ops.group_norm_grad(dy, x if ck is None else ck, stats, groups, w, bias, "silu")
+    s = _shape(batch, spatial, channels, groups, type=b.CMP_TYPE_F)
+    stream = torch.cuda.current_stream().cuda_stream
+    fmt = 1 if save == "e4m3" else 0
+
+    def within(need, call):
+        buf = torch.full((4096 + (need + 15) // 16 * 16 + 4096,), 0xa5, dtype=torch.uint8, device="cuda")
+        assert call(buf.data_ptr() + 4096 if need else None, need) == b.CMP_OK
+        torch.cuda.synchronize()
+        assert bool((buf[:4096] == 0xa5).all()) and bool((buf[4096 + need:] == 0xa5).all())
+
+    for with_stats in (True, False):
+        y2, stats2 = torch.zeros_like(y), torch.zeros_like(stats)
+        buf = None if ck is None else torch.zeros_like(ck.buf)
+        within(b.cmp_group_norm_forward_work(s, group), lambda p, n: b.cmp_group_norm_forward(
+            0, s, x.data_ptr(), w.data_ptr(), bias.data_ptr(), y2.data_ptr(), stats2.data_ptr() if with_stats else None, fmt, group,
+            None if ck is None else buf.data_ptr(), 0 if ck is None else buf.numel(), p, n, stream))
+        assert torch.equal(y2, y) and torch.equal(stats2, stats if with_stats else torch.zeros_like(stats))
+        assert ck is None or torch.equal(buf, ck.buf)
+    for want_w, want_b in ((True, True), (True, False), (False, True), (False, False)):
+        dx2, dw2, db2 = torch.zeros_like(dx), torch.zeros_like(dw), torch.zeros_like(db)
+        within(b.cmp_group_norm_grad_work(s, want_w or want_b), lambda p, n: b.cmp_group_norm_grad(
+            0, s, dy.data_ptr(), None if ck is not None else x.data_ptr(), fmt, group or 64, None if ck is None else ck.buf.data_ptr(),
+            0 if ck is None else ck.nbytes, w.data_ptr(), bias.data_ptr(), stats.data_ptr(), dx2.data_ptr(), dw2.data_ptr() if want_w else None,
+            db2.data_ptr() if want_b else None, p, n, stream))
+        assert torch.equal(dx2, dx)
+        assert torch.equal(dw2, dw if want_w else torch.zeros_like(dw)) and torch.equal(db2, db if want_b else torch.zeros_like(db))
+
+
+@pytest.mark.gpu
+def test_memory_of_normed_tokens():
+    """16384 tokens of 512 channels: a forward pass allocates its output and statistics, a backward pass without parameters dx."""
+    x = torch.randn(16384, 1, 512, device="cuda").bfloat16()
+    ops.group_norm(x, 32)
+
+    def more(call):
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        torch.cuda.reset_peak_memory_stats()
+        out = call()
+        return out, torch.cuda.max_memory_allocated() - before
+    (y, stats, _), used = more(lambda: ops.group_norm(x, 32))
+    assert used <= 2 * x.numel() + 16 * 16384 * 32 + (1 << 20)
+    _, used = more(lambda: ops.group_norm_grad(x, x, stats, 32, params=False))
+    assert used <= 2 * x.numel() + (1 << 20)
