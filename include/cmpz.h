@@ -349,7 +349,7 @@ int cmp_byte_load(int device, const cmp_byte_shape *shape, const void *d_ck, siz
  * summed in fp32 (fp16 and fp32 values of dY enter as the sum of two or three bf16 numbers, parts below 2^-126 may
  * be lost); each result is rounded once to out_type.  rows = 0 gives zeros.
  * d_work: cmp_byte_linear_grad_work bytes (it may be 0), aligned to 16, used during the call only; too few bytes
- * are CMP_E_NOSPACE.  cols and ld_dy above 2^24 and more than 2^36 values in dW are refused (CMP_E_ARG). */
+ * are CMP_E_NOSPACE.  cols and ld_dy above 2^24 and more than 2^36 values in dW are refused (CMP_E_ARG; 0 bytes of workspace). */
 size_t cmp_byte_linear_grad_work(const cmp_byte_shape *shape, uint64_t outs, uint32_t type);
 int cmp_byte_linear_grad(int device, const cmp_byte_shape *shape, const void *d_ck, size_t bytes, const void *d_dy, uint32_t type,
                          uint64_t outs, uint64_t ld_dy, void *d_dw, void *d_db, uint32_t out_type, int accumulate, void *d_work,

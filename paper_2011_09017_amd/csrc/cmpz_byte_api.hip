@@ -10,6 +10,7 @@ using namespace cmpz;
 namespace {
 
 constexpr uint64_t kMost = (1ull << 31) - 1;           // rows, columns, positions
+constexpr uint64_t kMostWide = 1ull << 24;             // a product's columns and rows of dY: offsets within 32 rows are kept in 32 bits
 
 struct DeviceGuard {
     int prev = -1;
@@ -36,6 +37,12 @@ bool shape_ok(const cmp_byte_shape *s)
 {
     return s && s->rows <= kMost && s->cols <= kMost && (s->format == CMP_BYTE_INT || s->format == CMP_BYTE_FLOAT) &&
            (s->group == 32 || s->group == 64 || s->group == 128);
+}
+
+// Workgroups of a product are counted by a launch.
+bool product_ok(const cmp_byte_shape &s, uint64_t outs)
+{
+    return s.cols <= kMostWide && outs <= kMostWide && outs * s.cols <= 1ull << 36;
 }
 
 uint32_t gshift_of(uint32_t group) { return group == 32 ? 5u : group == 64 ? 6u : 7u; }
@@ -171,7 +178,7 @@ int cmp_byte_load(int device, const cmp_byte_shape *shape, const void *d_ck, siz
 
 size_t cmp_byte_linear_grad_work(const cmp_byte_shape *shape, uint64_t outs, uint32_t type)
 {
-    if (!shape_ok(shape) || outs > kMost || type > CMP_TYPE_BF) return 0;
+    if (!shape_ok(shape) || !product_ok(*shape, outs) || type > CMP_TYPE_BF) return 0;
     return (size_t)linear_grad_work(shape->rows, shape->cols, outs, type);
 }
 
@@ -180,10 +187,8 @@ int cmp_byte_linear_grad(int device, const cmp_byte_shape *shape, const void *d_
                          size_t work_bytes, void *stream)
 {
     LinearGradArgs a{};
-    if (!shape_ok(shape) || outs > kMost || ld_dy < outs || type > CMP_TYPE_BF) return CMP_E_ARG;
+    if (!shape_ok(shape) || !product_ok(*shape, outs) || ld_dy < outs || ld_dy > kMostWide || type > CMP_TYPE_BF) return CMP_E_ARG;
     if (out_type != type && out_type != CMP_TYPE_F) return CMP_E_ARG;
-    // offsets within 32 rows are kept in 32 bits, workgroups counted by a launch
-    if (ld_dy > (1u << 24) || shape->cols > (1u << 24) || outs * shape->cols > (1ull << 36)) return CMP_E_ARG;
     const uint32_t es = type_bytes(type), os = type_bytes(out_type);
     if (shape->rows && outs && (!d_dy || misaligned(d_dy, es))) return CMP_E_ARG;
     if (shape->cols && outs && (!d_dw || misaligned(d_dw, os))) return CMP_E_ARG;

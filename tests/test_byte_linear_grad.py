@@ -223,3 +223,19 @@ def test_refusals_on_the_gpu():
                  lambda: ops.byte_linear_grad(dy, ck, out=f, dtype=torch.bfloat16)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("rows,cols,outs", [(64, 2 ** 31 - 1, 2 ** 31 - 1), (64, 2 ** 24 + 1, 8), (1000, 2 ** 31 - 1, 64), (10 ** 6, 2 ** 20, 2 ** 20),
+                                            (64, 64, 2 ** 31 - 1), (64, 2 ** 12, 2 ** 24 + 64), (0, 2 ** 31 - 1, 2 ** 31 - 1)])
+def test_no_workspace_for_sizes_that_are_refused(rows, cols, outs):
+    """The query knows the limits of the call: no plan is made for a product that is refused."""
+    s, P = binding.cmp_byte_shape(rows, cols, 0, 64), 4096
+    assert binding.cmp_byte_linear_grad_work(s, outs, 0) == 0
+    assert binding.cmp_byte_linear_grad(0, s, P, 1 << 62, P, 0, outs, outs, P, None, 0, False, P, 1 << 62, 0) == binding.CMP_E_ARG
+
+
+def test_the_largest_products_have_a_plan():
+    for cols, outs in ((2 ** 24, 2 ** 12), (2 ** 12, 2 ** 24), (2 ** 24, 8), (1, 2 ** 24), (2 ** 18 + 1, 2 ** 17 + 2 ** 16)):
+        for rows in (0, 1, 2 ** 31 - 1):
+            for kind in (0, 1, 2):
+                assert binding.cmp_byte_linear_grad_work(binding.cmp_byte_shape(rows, cols, 0, 32), outs, kind) < 2 ** 45
