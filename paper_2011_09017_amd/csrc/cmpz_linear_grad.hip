@@ -607,7 +607,8 @@ JoinJob join_job(const float *w, uint32_t count, uint64_t n, void *out)
     return j;
 }
 
-// Tiles of dW that a workgroup may take, its sets of waves, how many such workgroups a CU holds, and what a stage (32 rows
+// Tiles of dW that a workgroup may take, its sets of waves, how many such workgroups a CU holds (with three terms of dY one
+// of any tile: the smallest takes 96 KB of LDS then), and what a stage (32 rows
 // of each set) takes with w of them on it, in ns, for t terms: a0 + a1 * t + (b0 + b1 * t) * w.  Fitted to 8192 and 16384 rows, all
 // CUs busy (ns measured / fitted for bf16, fp16, fp32): 256 x 256: 980 / 975, 1740 / 1760, 2550 / 2545; 128 x 128: 707 / 707, 1205 /
 // 1199, 1692 / 1691; 64 x 256: 884 / 882, 1210 / 1254, 1631 / 1626; 64 x 64, two of them: 801 / 800, 1120 / 1120, one: 564 / 560, fp32
@@ -618,6 +619,7 @@ constexpr Tile kTiles[] = {{256, 256, 1, 1, 190, 785, 0, 0}, {128, 128, 2, 1, 21
                            {64, 64, 2, 2, 380, -60, 50, 190}};
 constexpr int kTileCount = 4, kFewOutputs = kTileCount;
 
+uint32_t resident_of(const Tile &t, uint32_t type) { return type == kTypeF32 ? 1u : t.resident; }
 bool few_outputs(uint64_t cols, uint64_t outs) { return outs < 8 || cols == 0; }
 
 // Time of the launches in ns, roughly: what the choice between tiles and numbers of ranges goes by.
@@ -626,10 +628,10 @@ double cost_of(const Tile &t, uint64_t rows, uint64_t cols, uint64_t outs, uint3
     const double terms = type == kTypeBF16 ? 1 : type == kTypeF16 ? 2 : 3;
     const double tiles = (double)((outs + t.n - 1) / t.n) * (double)((cols + t.k - 1) / t.k);
     const double per_cu = std::ceil(tiles * (double)splits / 256.0);
-    const double full = std::floor(per_cu / t.resident), rest = per_cu - full * t.resident;
+    const double resident = resident_of(t, type), full = std::floor(per_cu / resident), rest = per_cu - full * resident;
     auto stage = [&](double w) { return w > 0 ? t.a0 + t.a1 * terms + (t.b0 + t.b1 * terms) * w : 0.0; };
     const double stages = std::ceil((double)rows / kStep / (double)(splits * t.sets)) + 3;        // and what a workgroup begins with
-    const double body = stages * (full * stage(t.resident) + stage(rest));
+    const double body = stages * (full * stage(resident) + stage(rest));
     const double memory = (double)rows * ((double)outs * type_bytes(type) + (double)cols) / 5000.0;    // at 5 TB/s
     const double results = (double)t.n * t.k * (splits > 1 ? 4 : 2) * per_cu / 40.0;                   // stores at 40 B/ns per CU
     return (body > memory ? body : memory) + results + (splits > 1 ? 3000.0 + (double)splits * outs * cols * 4.0 / 5000.0 : 0.0);
@@ -654,10 +656,10 @@ Choice choose(uint64_t rows, uint64_t cols, uint64_t outs, uint32_t type)
         for (int i = 0; i < kTileCount; ++i) {
             const uint64_t tiles = ((outs + kTiles[i].n - 1) / kTiles[i].n) * ((cols + kTiles[i].k - 1) / kTiles[i].k);
             if (tiles > (1u << 22)) continue;                             // threads of a launch are counted with 32 bits
-            // one range, and as many as fill a quarter of the CUs, half of them, all of them once, twice, ...
-            for (uint64_t fill : {0ull, 64ull, 128ull, 256ull, 512ull, 768ull, 1024ull}) {
+            // one range, and as many as fill a quarter of the CUs, half of them, all of them once and, where two fit, twice
+            for (uint64_t fill : {0ull, 64ull, 128ull, 256ull, 512ull}) {
                 uint64_t k = fill / tiles;
-                if (fill && (k < 2 || fill > 256ull * kTiles[i].resident)) continue;
+                if (fill && (k < 2 || fill > 256ull * resident_of(kTiles[i], type))) continue;
                 if (k > steps / (4 * kTiles[i].sets)) k = steps / (4 * kTiles[i].sets);   // no fewer than four stages each
                 if (k < 1) k = 1;
                 const double t = cost_of(kTiles[i], rows, cols, outs, type, k);

@@ -239,3 +239,12 @@ def test_the_largest_products_have_a_plan():
         for rows in (0, 1, 2 ** 31 - 1):
             for kind in (0, 1, 2):
                 assert binding.cmp_byte_linear_grad_work(binding.cmp_byte_shape(rows, cols, 0, 32), outs, kind) < 2 ** 45
+
+
+@pytest.mark.parametrize("rows,cols,outs", [(183177, 44, 401), (56113, 54, 574), (190837, 53, 166), (123784, 24, 512)])
+def test_ranges_of_fp32_fill_the_chip_once(rows, cols, outs):
+    """Three terms of dY leave a CU one workgroup of 64 x 64 results (96 KB of LDS each), 256 of them on the chip: the ranges of
+    rows, counted by their partial sums of dW and db, are no more than that."""
+    work = binding.cmp_byte_linear_grad_work(binding.cmp_byte_shape(rows, cols, 0, 64), outs, binding.CMP_TYPE_F)
+    ranges, rest = divmod(work, 4 * outs * (cols + 1))
+    assert rest == 0 and 2 <= ranges <= 256 // -(-outs // 64)
