@@ -321,3 +321,42 @@ def test_a_norm_that_nothing_learns_from_stores_nothing(learns, monkeypatch):
         ts[learns - 1].requires_grad_()
     y = group_norm(ts[0], 4, ts[1], ts[2], fmt="e4m3")
     assert asked == ["e4m3" if learns else None] and y.requires_grad == bool(learns)
+
+
+@pytest.mark.gpu
+def test_shared_checkpoints_replay_from_a_graph():
+    """Three projections under the hooks and three with one checkpoint, forward and backward, captured once; every replay on
+    changed inputs, with eager steps between, gives the eager results."""
+    from paper_2011_09017_amd.autograd import linear
+    gen = torch.Generator().manual_seed(11)
+    ws = [torch.nn.Parameter(torch.randn(64, 256, generator=gen).to(DEV, torch.bfloat16)) for _ in range(3)]
+    sets = [[torch.randn(4, 32, n, generator=gen).to(DEV, torch.bfloat16) for n in (256, 64)] for _ in range(3)]
+    held = ByteCheckpoints("int8", 64, min_numel=1 << 10)
+
+    def step(x, dy):
+        x = x.detach().requires_grad_()
+        with held.hooks():
+            ys = [F.linear(x * 2, w) for w in ws[:1]] + [F.linear(x, w) for w in ws]
+        ck = ops.byte_store(x.detach())
+        ys += [linear(x, w, held=ck) for w in ws]
+        return [y.detach() for y in ys] + list(torch.autograd.grad(ys, [x, *ws], [dy] * len(ys)))
+
+    want = [[t.clone() for t in step(*s)] for s in sets]
+    ins = [t.clone() for t in sets[0]]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(*ins)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        outs = step(*ins)
+    for v in (1, 2, 0, 1):
+        for a, s in zip(ins, sets[v]):
+            a.copy_(s)
+        g.replay()
+        torch.cuda.synchronize()
+        for t, u in zip(outs, want[v]):
+            assert torch.equal(t, u)
+        step(*sets[(v + 1) % 3])
+        torch.cuda.synchronize()

@@ -123,3 +123,59 @@ def test_first_value_far_from_the_others(batch, spatial, channels, groups):
     dy = torch.randn(batch, spatial, channels, generator=gen).cuda()
     w, b = (1 + 0.5 * torch.randn(channels, generator=gen)).cuda(), (0.5 * torch.randn(channels, generator=gen)).cuda()
     _check(x.cuda(), dy, groups, w, b, "silu")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("spatial", [40, 3000])
+@pytest.mark.parametrize("channels,groups", [(64, 8), (60, 4), (40, 20)])
+def test_groups_far_from_zero_beside_others(spatial, channels, groups):
+    """One group of a workgroup far from zero, one spoilt by a NaN, one by an infinity: the others and the far one are right, and
+    the NaNs stay in their groups."""
+    gen = torch.Generator().manual_seed(4)
+    per = channels // groups
+    x = torch.randn(2, spatial, channels, generator=gen)
+    x[0, :, per:2 * per] += 1e5
+    x[1, 3, 2 * per] = float("nan")
+    x[1, spatial - 1, 4 * per - 1] = float("inf")
+    x = x.cuda()
+    y, stats, _ = ops.group_norm(x, groups)
+    bad = torch.zeros(2, 1, channels, dtype=torch.bool)
+    bad[1, :, 2 * per:4 * per] = True
+    assert torch.equal(torch.isnan(y).cpu(), bad.expand_as(y))
+    xd = torch.where(bad, torch.zeros(1, dtype=torch.float64), x.double().cpu())
+    want, mean, rstd, _ = ref.norm(xd, groups, torch.ones(channels, dtype=torch.float64), torch.zeros(channels, dtype=torch.float64), EPS, "none")
+    low = 2.0 ** -23 * _wide(mean.abs() * rstd, 2, channels)
+    good = torch.where(bad, want, y.double().cpu())
+    assert bool(((good - want).abs() <= 2.0 ** -21 * (want.abs() + low) + 2.0 ** -24 * want.abs() + 1e-37).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("spatial", [49, 3000])
+def test_replays_near_and_far_from_zero(spatial):
+    """Captured once on values near zero, replayed on values far from it and back: the eager results every time."""
+    gen = torch.Generator().manual_seed(5)
+    sets = [[(far + torch.randn(3, spatial, 96, generator=gen)).cuda(), torch.randn(3, spatial, 96, generator=gen).cuda()] for far in (0.0, 1e4, 3e6)]
+    w, b = torch.rand(96, generator=gen).cuda() + 0.5, torch.randn(96, generator=gen).cuda()
+
+    def step(x, dy):
+        y, stats, _ = ops.group_norm(x, 8, w, b, EPS, "silu")
+        return [y, stats, *ops.group_norm_grad(dy, x, stats, 8, w, b, "silu")]
+    want = [[t.clone() for t in step(*s)] for s in sets]
+    ins = [t.clone() for t in sets[0]]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(*ins)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        outs = step(*ins)
+    for v in (1, 0, 2, 1, 0):
+        for a, s in zip(ins, sets[v]):
+            a.copy_(s)
+        g.replay()
+        torch.cuda.synchronize()
+        for t, u in zip(outs, want[v]):
+            assert torch.equal(t, u)
+        step(*sets[(v + 1) % 3])
+        torch.cuda.synchronize()
