@@ -372,7 +372,8 @@ int cmp_byte_linear_grad(int device, const cmp_byte_shape *shape, const void *d_
  * The statistics are those of the input itself, so the error of a code enters h divided by the group's deviation: a norm
  * whose deviation is not well above the steps 2^e of its checkpoint (groups of a few equal values, channels of very
  * different sizes in one scale group) is better kept as d_x.  The derivative of CMP_ACT_RELU at 0 is 0.  Sums run over
- * fp32 or fp64 in an order that the sizes fix.
+ * fp32 or fp64 in an order that the sizes fix; those of mean and variance are taken a second time, about a value near the mean,
+ * by workgroups that find the variance lost in them, so that no error grows with mean / deviation.
  * A NaN or an infinity in x spoils its group, as the formulas have it.  With batch or spatial 0 nothing is written
  * but zeros in dgamma and dbeta.  d_y must not overlap d_x, nor d_dx d_dy. */
 #define CMP_ACT_NONE 0u

@@ -13,10 +13,14 @@
 // position; sums are kept per channel and thread and joined per channel, then per group, in LDS.
 //
 // Measured on bf16 with int8 codes, SiLU: 256 x 12544 x 64 in 8 groups (411 MB a tensor, copies run at 5.16 TB/s): forward sums
-// 104 us (3.9 TB/s), apply 215 (1031 MB in all, 4.8); backward sums 176 (3.5: the sigmoid and the codes' expansion on 16
-// values a lane beside 48 bytes of loads), apply 202 (5.1); counters show no byte read twice.  One pass, 256 x 49 x 512 fp32:
-// 17.3 and 22.9 us (3.4 and 2.5 TB/s): all its workgroups are on the chip at once, loading, adding and storing at the same
-// time; one sample of 49 x 512 bf16: 5.9 us, latency.
+// 103 us (4.0 TB/s), apply 222 (1031 MB in all, 4.6); backward sums 179 (3.5: the sigmoid and the codes' expansion on 16
+// values a lane beside 48 bytes of loads), apply 203 (5.1); counters show no byte read twice.  One pass, 256 x 49 x 512 fp32:
+// 18.0 and 22.2 us (3.3 and 2.6 TB/s): all its workgroups are on the chip at once, loading, adding and storing at the same
+// time; one sample of 49 x 512 bf16: 6.3 us, latency.
+//
+// All are compiled for 1024 threads, so for 128 registers.  One-pass backward kernels of vectors that cross groups (ONE false) spill
+// up to 54 of them (ReLU), 22 (SiLU) and 14 (none): 256 x 49 x 480 in 32 groups, ReLU fp32 with int8 codes, takes 40.3 us
+// backward where 512 channels take 26.0.
 #include "cmpz_byte.h"
 
 #include <type_traits>
@@ -169,7 +173,7 @@ __device__ __forceinline__ void join_channels(V *s, const V (&v)[8], const V (&w
 }
 
 // Lanes that add up `items` values: a whole wave, or for few a power of two of it, so that a wave takes several groups at once
-// (65536 x 1 x 512 in 32 groups, forward: 880 us with a wave to a group, 140 so; 64 x 3136 x 256 in 256: 117 and 83).
+// (65536 x 1 x 512 in 32 groups, forward: 880 us with a wave to a group, 139 so; 64 x 3136 x 256 in 256: 117 and 83).
 __device__ __forceinline__ uint32_t lanes_of(uint32_t items)
 {
     uint32_t w = 64u;

@@ -8,9 +8,12 @@
 // Both operands are reduced along their rows, so both are read transposed from LDS.  Measured, rows x cols x outs of
 // 8192 x 4096 x 4096 on random values: int8 with bf16 252 us (1.09 PFLOP/s), e4m3 226, fp16 450 and fp32 660 (two and three
 // terms); 16384 x 4096 x 8192 e4m3 877 us (1.25 PFLOP/s); 8192^3 as A^T B from bf16 in memory the library reaches 1.12.
-// A stage of 32 rows takes 0.98 us at 256 x 256, of which the matrix instructions are busy for half; beside them lie the
-// expansion (int8: 12 % over e4m3) and 3.4 reads of the operands through eight L2 caches (340 MB, 1.35 TB/s: no bound).
-// Operands of zeros take 219 us: part of the rest is power.
+// A stage of 32 rows takes 0.98 us at 256 x 256.  Counters of 8192 x 4096 x 4096 (int8, e4m3): matrix units busy for 50 and 59 % of
+// the clock cycles, LDS for 39 and 45 (a sixth of that are bank conflicts), so neither is the bound: all eight waves pass one
+// barrier a stage and are in the same phase together, and the two units work in turn.  Beside them lie the expansion (int8: 12 %
+// over e4m3) and 3.4 reads of the operands through eight L2 caches (340 MB, 1.35 TB/s: no bound).  Operands of zeros take 219 us:
+// part of the rest is power.  fp16 could do with one product to a value (x' is an fp16 number too but in groups of extreme
+// exponents), at half of its matrix work; the split is the one that needs no look at the exponents.
 #include "cmpz_byte.h"
 
 #include <cmath>
