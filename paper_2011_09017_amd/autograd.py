@@ -206,7 +206,8 @@ class ByteCheckpoints:
     """saved_tensors_hooks that hold every saved fp32, fp16 or bf16 tensor as a byte checkpoint, whatever its shape and
     whatever the order of its dimensions in memory (channels last included; groups run along the dimension that is
     dense).  A graph can be walked backward as often as autograd allows: checkpoints are only read.  What several
-    operations of a forward pass save (the input of three projections) is held once, as autograd itself has it.
+    operations of a forward pass save (the input of three projections) is held once, as autograd itself has it (changes in
+    between that torch does not count, through raw pointers, are not seen).
 
     fmt, group: see operators.byte_store.  min_numel: smaller tensors are saved as they are, and so are parameters
     (torch.nn.Parameter, frozen ones too), tensors named to skip_parameters, views of either and copies of them in another type or
@@ -222,19 +223,20 @@ class ByteCheckpoints:
     def __init__(self, fmt: str = "int8", group: int = 64, min_numel: int = 1 << 14):
         operators._byte_shape(0, 0, fmt, group)                       # refuses what byte_store would refuse later
         self.fmt, self.group, self.min_numel = fmt, int(group), int(min_numel)
-        self._named = []                        # weak references: an address means a tensor as long as that lives
+        self._named = []                        # weak references: an address means what was named as long as that lives
         self._skip = set()                      # their storages
         self._by_memory = {}                    # what memory held -> (weak ref of its storage, of its checkpoint's bytes), current forward pass
         self.stats = {"packed": 0, "shared": 0, "raw_bytes": 0, "held_bytes": 0, "passed_through": 0}
 
     def skip_parameters(self, params: Iterable[torch.Tensor]) -> None:
-        self._named += [weakref.ref(p) for p in params]
+        # of the tensor, whose storage may change, and of the storage, which outlives a view that only served to name it
+        self._named += [(weakref.ref(p), StorageWeakRef(p.untyped_storage()), _storage(p)) for p in params]
         self._find_named()
 
     def _find_named(self) -> None:
-        alive = [(ref, ref()) for ref in self._named]
-        self._named = [ref for ref, t in alive if t is not None]
-        self._skip = {_storage(t) for _, t in alive if t is not None}
+        self._named = [n for n in self._named if n[0]() is not None or not n[1].expired()]
+        tensors = [n[0]() for n in self._named]
+        self._skip = {_storage(t) for t in tensors if t is not None} | {at for _, storage, at in self._named if not storage.expired()}
 
     def _is_weight(self, t: torch.Tensor) -> bool:
         def known(v):

@@ -360,3 +360,17 @@ def test_shared_checkpoints_replay_from_a_graph():
             assert torch.equal(t, u)
         step(*sets[(v + 1) % 3])
         torch.cuda.synchronize()
+
+
+def test_names_given_by_a_temporary_last_as_long_as_their_memory():
+    """A view or a detached alias that nobody keeps names the tensor behind it."""
+    for alias in (lambda t: t.t(), lambda t: t.data, lambda t: t.detach()[3:], lambda t: t.view(-1)):
+        w = torch.randn(48, 64)
+        held = _Recorder()
+        held.skip_parameters(alias(t) for t in [w])
+        with held.hooks():
+            assert held._is_weight(w) and held._is_weight(w.t())
+        at = w.untyped_storage().data_ptr()
+        del w
+        with held.hooks():
+            assert at not in held._skip
