@@ -200,6 +200,7 @@ def byte_linear_grad(dy: torch.Tensor, ck: ByteCheckpoint, bias: bool = False, d
 def _norm_plan(batch: int, spatial: int, channels: int, groups: int, kind: int, act: str, eps: float, backward: bool, part: int):
     """(the C shape, bytes of the workspace): depend on sizes only and are read only."""
     _refuse(not 0 <= groups < 1 << 32 or channels >= 1 << 32, f"group norm: {groups} groups of {channels} channels")   # fields of 32 bits
+    _call(binding.CMP_E_ARG if groups > channels else binding.CMP_OK, "cmp_group_norm")     # before statistics of so many are allocated
     shape = binding.cmp_norm_shape(batch, spatial, channels, groups, kind, _ACTS[act], eps)
     return shape, (binding.cmp_group_norm_grad_work if backward else binding.cmp_group_norm_forward_work)(shape, part)
 

@@ -125,3 +125,12 @@ def test_memory_of_normed_tokens():
     assert used <= 2 * x.numel() + 16 * 16384 * 32 + (1 << 20)
     _, used = more(lambda: ops.group_norm_grad(x, x, stats, 32, params=False))
     assert used <= 2 * x.numel() + (1 << 20)
+
+
+def test_more_groups_than_channels_are_refused_before_anything_is_allocated():
+    """Statistics of 2^32 - 1 groups would take 64 GB."""
+    for groups in (9, (1 << 32) - 1):
+        with pytest.raises(b.CmpError):
+            ops.group_norm(torch.empty(1, 3, 8), groups)
+        with pytest.raises(b.CmpError):
+            ops.group_norm_grad(torch.empty(1, 3, 8), torch.empty(1, 3, 8), torch.empty(0), groups)
